@@ -246,6 +246,85 @@ int naut_attn_decode_static(const void* q, const void* k, const void* v, void* o
 size_t naut_attn_decode_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, int D);
 
 /*
+ * The same operator on packed sequences: n sequences of different lengths lie back to back, as a serving engine batches
+ * prompts.  q and o are [Tq][Hq][D], k and v [Tk][Hkv][D], lse [Hq][Tq] (fp32, may be NULL); sequence i owns the rows
+ * cu_q[i] .. cu_q[i+1]-1 of q and o and cu_k[i] .. cu_k[i+1]-1 of k and v.  cu_q and cu_k are DEVICE memory, n + 1 int each,
+ * non-decreasing (the same pointer may serve as both); the host reads neither, so a captured call follows what they hold
+ * when it is replayed.  With Sq queries and Sk keys in a sequence, query i sees every key, or with `causal` the keys
+ * 0 .. Sk-Sq+i: its queries are its last Sq positions, and Sq == Sk is the mask of naut_attn_fwd.  A row that sees nothing
+ * (no keys, or with `causal` fewer keys than queries) has o = 0 and lse = -inf.  Lengths of 0 and 1 are ordinary.  Rows of o
+ * and lse that belong to no sequence are left as they are, and rows of k and v outside a sequence do not reach its results,
+ * whatever they hold.  A pair of offsets that falls, is negative or passes Tq or Tk makes its sequence empty.
+ * `st` gives the head and sequence (row) strides in elements, by the rules of naut_attn_fwd_strided; the batch strides are not
+ * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Tq and Tk at most 2^30, n at most
+ * 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
+ */
+int naut_attn_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_q,
+                         const int* cu_k, int n, int Tq, int Tk, int Hq, int Hkv, int D, int causal, float scale,
+                         void* stream, int in_dtype, int out_dtype, const naut_strides* st);
+
+/*
+ * A key/value cache in 4 bits (OCP MXFP4).  A row of D values, D a multiple of 32 up to 256, is held in blocks of 32: value =
+ * code * 2^(byte - 127), the codes E2M1 (sign, then the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte with the even
+ * element in the low nibble, and one scale byte per block (1 .. 254; 255 is NaN and must not occur).  Row s of head h of
+ * sequence b has its D/2 code bytes at codes + b*c_b + h*c_h + s*c_s and its D/32 scale bytes at scales + b*s_b + h*s_h +
+ * s*s_s, for K and V alike.  codes are 16-byte aligned, their strides non-negative multiples of 16; the rows of scales
+ * are padded to naut_kv4_scale_bytes(D) = 2 (D <= 64), 4 (D <= 128) or 8 bytes (the rest of them is not looked at), to which
+ * scales and its strides are aligned.  c_s is at least D/2, s_s at least the padded row, both at most 2^23.  Everything is
+ * DEVICE memory of the caller.  At D = 128 a cached row takes 68 bytes, a 16-bit one 256.
+ */
+typedef struct {
+    void* k_codes;
+    void* k_scales;
+    void* v_codes;
+    void* v_scales;
+    long long c_b, c_h, c_s; /* strides of batch, head and position, in bytes: of both codes */
+    long long s_b, s_h, s_s; /* and of both scales */
+    int B, Hkv, S, D;        /* sequences, heads, positions that each has room for, head dimension */
+} naut_kv4_cache;
+
+/* Bytes that the scales of one row take (see naut_kv4_cache); 0 if D is unsupported.  Host only. */
+int naut_kv4_scale_bytes(int D);
+
+/*
+ * Writes T rows of k and v ([T][Hkv][D], in_dtype NAUT_BF16 or NAUT_F16) into the cache: row t goes to position slots[t] % S
+ * of sequence slots[t] / S; a slot below 0 or from B*S on is skipped, as the padding of a batch is.  slots is DEVICE memory, T
+ * int; no position may occur twice in one call.  The scale of a block is the least power of two 2^e with max|x| < 7 * 2^e (at
+ * which the largest value does not round past 6), but at most 2^125 (NAUT_F16: 2^13, so that every value is finite in the type) and at least 2^-126;
+ * codes are rounded to nearest, ties to the even code, and saturate.  Values must be finite.  `st` gives the head and
+ * sequence (row) strides of k and v in elements, non-negative multiples of 8 (NULL = contiguous; its other members are not looked at).
+ * k and v 16-byte aligned.  One kernel on `stream`.
+ */
+int naut_kv4_store(const void* k, const void* v, const naut_kv4_cache* cache, const int* slots, int T, int in_dtype,
+                   const naut_strides* st, void* stream);
+
+/*
+ * The reverse: rows of the cache as 16-bit values, exact in bf16 (NAUT_F16: scales above 2^13 count as 2^13, values below the
+ * type's range round), e.g. for naut_attn_fwd_packed when a cached conversation goes on.  A row whose slot is skipped is
+ * left as it is; a position may be read any number of times.  Strides of k and v positive multiples of 8, sequence strides at least D.
+ */
+int naut_kv4_load(void* k, void* v, const naut_kv4_cache* cache, const int* slots, int T, int out_dtype,
+                  const naut_strides* st, void* stream);
+
+/*
+ * Decode-time attention over such a cache, whose sequences may have different lengths: q and o are [B][Hq][Sq][D], lse
+ * [B][Hq][Sq] (fp32, may be NULL); sequence b has lens[b] keys (DEVICE memory, B int; NULL: S each; a length outside 0 .. S
+ * counts as the nearer of the two), and its Sq queries see all of them, or with `causal` query i the keys 0 .. lens[b]-Sq+i.
+ * A row that sees nothing has o = 0 and lse = -inf.  Both products run on the cache's values in the type of q (NAUT_F16 as in
+ * naut_kv4_load) with fp32 accumulation; the softmax runs in fp32.  The key axis is split by the lengths that the GPU finds,
+ * so that a captured call follows them; the partials live in `workspace` (DEVICE memory of the caller, 16-byte aligned, at least
+ * naut_attn_decode_kv4_workspace_bytes(...) bytes, overwritten, not shared by calls that may overlap).  One or two kernels.
+ * `st` gives the batch, head and sequence strides of q and o in elements by the rules of naut_attn_fwd_strided (NULL =
+ * contiguous; those of k and v are not looked at).  Types and scale as in naut_attn_decode_dt.
+ */
+int naut_attn_decode_kv4(const void* q, void* o, float* lse, const naut_kv4_cache* cache, const int* lens, int Hq, int Sq,
+                         int causal, float scale, void* workspace, size_t workspace_bytes, void* stream, int in_dtype,
+                         int out_dtype, const naut_strides* st);
+
+/* Bytes of workspace naut_attn_decode_kv4 needs for these sizes (S: the cache's); 0 if they are unsupported.  Host only. */
+size_t naut_attn_decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int Sq, int S, int D);
+
+/*
  * Measurement aid, not part of the attention path (the paper's evaluation, Section 6, reports throughput
  * against the hardware's capability; this gives the capability of the box at hand): a register-only loop of
  * the matrix instruction the bf16 kernels use (v_mfma_f32_32x32x16_bf16), `work_groups` work-groups of 8

@@ -28,13 +28,22 @@ NAUT_F32 = 2
 EXPORTS = ("naut_attn_fwd", "naut_attn_fwd_dt", "naut_last_error_string", "naut_version",
            "naut_attn_variant_name", "naut_attn_fwd_kernel_name", "naut_attn_key_groups", "naut_attn_fwd_fp8_key_groups", "naut_attn_decode", "naut_attn_decode_dt", "naut_attn_decode_workspace_bytes",
            "naut_attn_fwd_strided", "naut_attn_fwd_fp8", "naut_attn_decode_strided", "naut_attn_fwd_fp8_strided", "naut_attn_decode_fp8", "naut_attn_decode_fp8_strided",
-           "naut_attn_decode_static", "naut_probe_mfma")
+           "naut_attn_decode_static", "naut_probe_mfma", "naut_attn_fwd_packed", "naut_kv4_scale_bytes", "naut_kv4_store", "naut_kv4_load",
+           "naut_attn_decode_kv4", "naut_attn_decode_kv4_workspace_bytes")
 
 
 class NautStrides(ctypes.Structure):
     """Element strides of the batch, head and sequence axes of q, k, v, o (mirror of naut_strides)."""
     _fields_ = [(n, ctypes.c_longlong) for n in ("q_b", "q_h", "q_s", "k_b", "k_h", "k_s", "v_b", "v_h", "v_s",
                                                  "o_b", "o_h", "o_s")]
+
+
+class NautKv4Cache(ctypes.Structure):
+    """Mirror of naut_kv4_cache."""
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k_codes", "k_scales", "v_codes", "v_scales")]
+                + [(n, ctypes.c_longlong) for n in ("c_b", "c_h", "c_s", "s_b", "s_h", "s_s")]
+                + [(n, ctypes.c_int) for n in ("B", "Hkv", "S", "D")])
+
 
 _lib = None
 
@@ -92,6 +101,19 @@ def load(path: str):
     L.naut_probe_mfma.argtypes = [vp, sz, ci, ci, ci, vp]
     L.naut_attn_decode_static.restype = ci
     L.naut_attn_decode_static.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp]
+    st, kv = ctypes.POINTER(NautStrides), ctypes.POINTER(NautKv4Cache)
+    L.naut_attn_fwd_packed.restype = ci
+    L.naut_attn_fwd_packed.argtypes = [vp, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, ci, cf, vp, ci, ci, st]
+    L.naut_kv4_scale_bytes.restype = ci
+    L.naut_kv4_scale_bytes.argtypes = [ci]
+    L.naut_kv4_store.restype = ci
+    L.naut_kv4_store.argtypes = [vp, vp, kv, vp, ci, ci, st, vp]
+    L.naut_kv4_load.restype = ci
+    L.naut_kv4_load.argtypes = [vp, vp, kv, vp, ci, ci, st, vp]
+    L.naut_attn_decode_kv4.restype = ci
+    L.naut_attn_decode_kv4.argtypes = [vp, vp, vp, kv, vp, ci, ci, ci, cf, vp, sz, vp, ci, ci, st]
+    L.naut_attn_decode_kv4_workspace_bytes.restype = sz
+    L.naut_attn_decode_kv4_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
     return L
 
 
@@ -495,6 +517,157 @@ def naut_attn_decode_fp8_strided(q, k, v, o, lse, causal: bool, scale: float, de
                                           _stream_ptr(stream, q), _strides(q, k, v, o))
     if rc != NAUT_OK:
         raise NautError(rc, last_error_string())
+
+
+def _one_device(tensors):
+    """The device of all of them; an error where they are not on one GPU."""
+    device = tensors[0].device
+    for t in tensors:
+        if not t.is_cuda or t.device != device:
+            raise ValueError("all tensors must be on one GPU")
+    return device
+
+
+def _call(device, f, *args):
+    """f(*args) with `device` current (a launch goes to the current device), its status raised."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        rc = f(*args)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args)
+    if rc != NAUT_OK:
+        raise NautError(rc, last_error_string())
+
+
+def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float, stream=None):
+    """Attention forward on packed sequences of different lengths.
+
+    q,o [Tq,Hq,D]; k,v [Tk,Hkv,D] (the last axis contiguous, any head and row strides); lse contiguous fp32 [Hq,Tq] or
+    None; cu_q, cu_k contiguous int32 device tensors [n+1], the offsets of the n sequences' rows (they may be one tensor).
+    The queries of a sequence are the last positions of its keys.  Rows of no sequence are left as they are, a row that
+    sees no key gets o = 0 and lse = -inf.  Enqueues on `stream` and returns; the lengths are read on the GPU."""
+    import torch
+    for t in (q, k, v, o):
+        if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
+            raise ValueError("q, k, v, o must be 3-d with a contiguous last axis")
+    device = _one_device((q, k, v, o, cu_q, cu_k) if lse is None else (q, k, v, o, cu_q, cu_k, lse))
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    if k.shape != (Tk, Hkv, D) or v.shape != (Tk, Hkv, D) or o.shape != (Tq, Hq, D):
+        raise ValueError("shape mismatch between q, k, v, o")
+    if k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q, k, v must share one dtype")
+    if lse is not None and not (lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (Hq, Tq)):
+        raise ValueError("lse must be a contiguous fp32 device tensor [Hq,Tq]")
+    n = cu_q.numel() - 1
+    for t in (cu_q, cu_k):
+        if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() != n + 1 or n < 0:
+            raise ValueError("cu_q and cu_k must be contiguous int32 tensors of n + 1 offsets each")
+    st = NautStrides(0, q.stride(1), q.stride(0), 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0), 0, o.stride(1), o.stride(0))
+    _call(device, lib().naut_attn_fwd_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
+          None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, Tq, Tk, Hq, Hkv, D, int(bool(causal)),
+          float(scale), _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o), ctypes.byref(st))
+
+
+def kv4_scale_bytes(D: int) -> int:
+    """Bytes that the scales of one cached row take (0: unsupported head dimension)."""
+    return int(lib().naut_kv4_scale_bytes(D))
+
+
+class KV4Cache:
+    """A key/value cache in 4 bits: the caller's tensors, checked once.
+
+    k_codes, v_codes uint8 [B,Hkv,S,D/2]; k_scales, v_scales uint8 [B,Hkv,S,kv4_scale_bytes(D)]; the last axes contiguous,
+    the others with any strides (a sequence-major cache is `x.transpose(1, 2)`), the same for K and V."""
+
+    def __init__(self, k_codes, k_scales, v_codes, v_scales):
+        import torch
+        self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        for t in self.tensors:
+            if t.dtype != torch.uint8 or t.dim() != 4 or t.stride(3) != 1:
+                raise ValueError("codes and scales must be 4-d uint8 tensors with a contiguous last axis")
+        self.device = _one_device(self.tensors)
+        B, Hkv, S, half = k_codes.shape
+        self.B, self.Hkv, self.S, self.D = B, Hkv, S, 2 * half
+        if v_codes.shape != k_codes.shape or v_scales.shape != k_scales.shape or k_scales.shape != (B, Hkv, S, kv4_scale_bytes(self.D)):
+            raise ValueError("codes must be [B,Hkv,S,D/2] and scales [B,Hkv,S,kv4_scale_bytes(D)], D a multiple of 32 up to 256")
+        if v_codes.stride() != k_codes.stride() or v_scales.stride() != k_scales.stride():
+            raise ValueError("K and V must have the same strides")
+        self.struct = NautKv4Cache(*(t.data_ptr() for t in self.tensors), *k_codes.stride()[:3], *k_scales.stride()[:3], B, Hkv, S, self.D)
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, B: int, Hkv: int, S: int, D: int, device="cuda"):
+        """A cache of new tensors, [B,Hkv,S] in memory; nothing is in it yet."""
+        import torch
+        make = lambda n: torch.empty((B, Hkv, S, n), dtype=torch.uint8, device=device)
+        n = kv4_scale_bytes(D)
+        if n == 0:
+            raise ValueError("D must be a multiple of 32, at most 256")
+        return cls(make(D // 2), make(n), make(D // 2), make(n))
+
+
+def _kv4_rows(f, k, v, cache, slots, stream):
+    import torch
+    device = _one_device((k, v, slots))
+    if device != cache.device:
+        raise ValueError("all tensors must be on one GPU")
+    T = slots.numel()
+    for t in (k, v):
+        if t.dim() != 3 or t.shape != (T, cache.Hkv, cache.D) or t.stride(2) != 1 or t.dtype != k.dtype:
+            raise ValueError("k and v must be [T,Hkv,D] of one dtype with a contiguous last axis, T the number of slots")
+    if slots.dtype != torch.int32 or slots.dim() != 1 or not slots.is_contiguous():
+        raise ValueError("slots must be a contiguous int32 device tensor [T]")
+    st = NautStrides(0, 0, 0, 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0), 0, 0, 0)
+    _call(device, f, k.data_ptr(), v.data_ptr(), cache.ref, slots.data_ptr(), T, _torch_dtype_code(k), ctypes.byref(st),
+          _stream_ptr(stream, k))
+
+
+def naut_kv4_store(k, v, cache, slots, stream=None):
+    """Rows k, v [T,Hkv,D] (bf16 or f16) into a KV4Cache: row t becomes position slots[t] % S of sequence slots[t] // S.
+    slots: contiguous int32 device tensor [T]; a slot outside 0 .. B*S-1 (such as -1 for padding) is skipped, and none may
+    occur twice."""
+    _kv4_rows(lib().naut_kv4_store, k, v, cache, slots, stream)
+
+
+def naut_kv4_load(k, v, cache, slots, stream=None):
+    """The reverse of naut_kv4_store: rows of a KV4Cache into k, v [T,Hkv,D].  Rows whose slot is skipped are left as they are."""
+    _kv4_rows(lib().naut_kv4_load, k, v, cache, slots, stream)
+
+
+def decode_kv4_workspace_bytes(B: int, Hq: int, Hkv: int, Sq: int, S: int, D: int) -> int:
+    """Bytes of device workspace naut_attn_decode_kv4 needs (S: positions that the cache has room for; 0: unsupported)."""
+    return int(lib().naut_attn_decode_kv4_workspace_bytes(B, Hq, Hkv, Sq, S, D))
+
+
+def naut_attn_decode_kv4(q, o, lse, cache, lens, causal: bool, scale: float, workspace, stream=None):
+    """Decode-time attention over a KV4Cache: q,o [B,Hq,Sq,D] (the last Sq positions of each sequence; the last axis
+    contiguous), lse contiguous fp32 [B,Hq,Sq] or None, lens contiguous int32 device tensor [B], the keys that each sequence
+    has (None: S each), workspace contiguous, at least decode_kv4_workspace_bytes(...) bytes.  Enqueues on `stream`; the
+    lengths are read on the GPU."""
+    import torch
+    tensors = [q, o, workspace] + [t for t in (lse, lens) if t is not None]
+    device = _one_device(tensors)
+    if device != cache.device:
+        raise ValueError("all tensors must be on one GPU")
+    for t in (q, o):
+        if t.dim() != 4 or t.stride(3) != 1:
+            raise ValueError("q and o must be 4-d with a contiguous last axis")
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    B, Hq, Sq, D = q.shape
+    if o.shape != q.shape or B != cache.B or D != cache.D:
+        raise ValueError("shape mismatch between q, o and the cache")
+    if lse is not None and not (lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (B, Hq, Sq)):
+        raise ValueError("lse must be a contiguous fp32 device tensor [B,Hq,Sq]")
+    if lens is not None and not (lens.is_contiguous() and lens.dtype == torch.int32 and lens.shape == (B,)):
+        raise ValueError("lens must be a contiguous int32 device tensor [B]")
+    st = NautStrides(*q.stride()[:3], 0, 0, 0, 0, 0, 0, *o.stride()[:3])
+    _call(device, lib().naut_attn_decode_kv4, q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), cache.ref,
+          None if lens is None else lens.data_ptr(), Hq, Sq, int(bool(causal)), float(scale), workspace.data_ptr(),
+          workspace.numel() * workspace.element_size(), _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o),
+          ctypes.byref(st))
 
 
 def naut_probe_mfma(out, work_groups: int, trips: int, kind: int, stream=None) -> float:

@@ -100,6 +100,10 @@ struct Params {
     int cpr;       // real 16-byte chunks per row = head dimension / 8
 };
 
+}  // namespace naut_k
+#include "naut_packed.h"
+namespace naut_k {
+
 // The order of work-groups that keeps an XCD to few heads: work-groups are dealt to the 8 XCDs round-robin by block id, and
 // each XCD has its own L2.  Every XCD gets a contiguous run of an eighth of the (batch, head) pairs, in `groups` groups of
 // nearly one size, one group after the other, each with its heaviest (last) query tiles first.  Pairs that eight does not
@@ -175,8 +179,9 @@ struct XMfma<NAUT_F16> {
 // load (three launches at a time, before the clock falls, 5026 / 3922); the D = 128 kernel reaches 1150 to 1190.  D = 192,
 // 4x64/8 heads, S = 3835: 2106 / 1387 us.  Outputs are bit-identical (same tiles, same order).
 
-template <int D, int DT_IN, int DT_OUT, bool CAUSAL, int NWV = NWAVES, int NG = 1>
-__global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kernel_bm128(const Params p)
+// PACKED as in kernel 2.
+template <int D, int DT_IN, int DT_OUT, bool CAUSAL, int NWV = NWAVES, int NG = 1, bool PACKED = false>
+__global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kernel_bm128(const ParamsOf<PACKED> p)
 {
     using T = In<DT_IN>;
     constexpr int BM = NWV * 32;             // queries per work-group (hides the file-scope value)
@@ -217,36 +222,63 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 
     // Tile scheduler: heaviest (last) query tiles first; consecutive block ids walk the
     // (batch, head) axis so that each XCD (block id mod 8) keeps to a fixed subset of heads.
-    const int nbh = p.B * p.Hq;
-    const int nqt = NWV == 4 ? p.nqt : NWV == 8 ? p.nqt2 : (p.S + BM - 1) / BM;
-    const int bid = blockIdx.x;
-    int qt, bh;
-    if (NWV == 8) {
-        // About HEADS_AT_ONCE heads at a time in groups of nearly one size: a last group of one or two heads would start its
-        // heaviest tiles when everything else is done (D = 256, causal, S = 1536, 72 heads, nine to an XCD: eight and one 153
-        // us, nine 113; S = 2048, 136 heads: eight, eight and one 392, nine and eight 327; all at once costs 2 to 4 % of
-        // larger grids).
-        const int hpx = nbh >> 3;
-        const QueryTile t = tile_by_head(bid, nbh, nqt, hpx < HEADS_AT_ONCE ? 1 : (hpx + HEADS_AT_ONCE / 2) / HEADS_AT_ONCE);
+    int qt, hq, Sq, Sk;
+    long long q_first, k_first, v_first, o_first, lse_first;  // bytes (lse: values) to the sequence's first row
+    if constexpr (PACKED) {
+        const PackedTile t = packed_tile<BM>(p, blockIdx.x, lane);
+        if (t.qt < 0)
+            return;
         qt = t.qt;
-        bh = t.bh;
+        hq = t.hq;
+        Sq = t.Sq;
+        Sk = t.Sk;
+        if (Sk == 0 || (CAUSAL && (qt + 1) * BM + Sk <= Sq)) {
+            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, hq, t.q0 + qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
+            return;
+        }
+        q_first = (long long)t.q0 * p.q_rs;
+        k_first = (long long)t.k0 * p.k_rs;
+        v_first = (long long)t.k0 * p.v_rs;
+        o_first = (long long)t.q0 * p.o_rs;
+        lse_first = (long long)hq * p.Tq + t.q0;
     } else {
-        qt = nqt - 1 - bid / nbh;
-        bh = bid % nbh;
+        const int nbh = p.B * p.Hq;
+        const int nqt = NWV == 4 ? p.nqt : NWV == 8 ? p.nqt2 : (p.S + BM - 1) / BM;
+        const int bid = blockIdx.x;
+        int bh;
+        if (NWV == 8) {
+            // About HEADS_AT_ONCE heads at a time in groups of nearly one size: a last group of one or two heads would start its
+            // heaviest tiles when everything else is done (D = 256, causal, S = 1536, 72 heads, nine to an XCD: eight and one 153
+            // us, nine 113; S = 2048, 136 heads: eight, eight and one 392, nine and eight 327; all at once costs 2 to 4 % of
+            // larger grids).
+            const int hpx = nbh >> 3;
+            const QueryTile t = tile_by_head(bid, nbh, nqt, hpx < HEADS_AT_ONCE ? 1 : (hpx + HEADS_AT_ONCE / 2) / HEADS_AT_ONCE);
+            qt = t.qt;
+            bh = t.bh;
+        } else {
+            qt = nqt - 1 - bid / nbh;
+            bh = bid % nbh;
+        }
+        const int b = bh / p.Hq;
+        hq = bh % p.Hq;
+        Sq = Sk = p.S;
+        q_first = b * p.q_bs;
+        k_first = b * p.k_bs;
+        v_first = b * p.v_bs;
+        o_first = b * p.o_bs;
+        lse_first = (long long)bh * p.S;
     }
-    const int b = bh / p.Hq;
-    const int hq = bh % p.Hq;
+    const int ahead = PACKED ? Sk - Sq : 0;  // keys before the first query's own
     const int hk = hq / (p.Hq / p.Hkv);
-    const int S = p.S;
 
-    const unsigned char* qg = (const unsigned char*)p.q + b * p.q_bs + hq * p.q_hs;
-    const unsigned char* kg = (const unsigned char*)p.k + b * p.k_bs + hk * p.k_hs;
-    const unsigned char* vg = (const unsigned char*)p.v + b * p.v_bs + hk * p.v_hs;
+    const unsigned char* qg = (const unsigned char*)p.q + q_first + hq * p.q_hs;
+    const unsigned char* kg = (const unsigned char*)p.k + k_first + hk * p.k_hs;
+    const unsigned char* vg = (const unsigned char*)p.v + v_first + hk * p.v_hs;
     const int cpr = p.cpr;
 
     const int q_wave0 = qt * BM + wave * 32;  // first query of this wavefront
     const int my_q = q_wave0 + l32;           // the query this lane owns
-    const int my_q_ld = my_q < S ? my_q : S - 1;
+    const int my_q_ld = my_q < Sq ? my_q : Sq - 1;
 
     // Q^T fragments (MFMA B operand): lane holds q[my_q][16*ks + 8*h .. +8].
     i32x4_t qf[KS];
@@ -278,7 +310,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
     if constexpr (WIDE)
         pin_q(cpr);
 
-    const int kv_end = CAUSAL ? (S < (qt + 1) * BM ? S : (qt + 1) * BM) : S;
+    const int kv_end = CAUSAL ? (Sk < (qt + 1) * BM + ahead ? Sk : (qt + 1) * BM + ahead) : Sk;
     const int ntiles = (kv_end + BN - 1) / BN;
 
     // Lane i of direct load n fills physical chunk P = (wave*LDW + n)*64 + i of the tile, so it fetches the
@@ -314,7 +346,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
             wv_col[n] += wv_row[n] * p.v_rs;
         }
     }
-    const int last_tile = (S + BN - 1) / BN - 1;  // of the sequence: the only one that can be ragged
+    const int last_tile = (Sk + BN - 1) / BN - 1;  // of the sequence: the only one that can be ragged
     const int my_tiles = (ntiles - grp + NG - 1) / NG;  // of this key group: grp, grp + NG, ...
     // The address of a load is the tile's base, a 64-bit wave-uniform pointer, plus a 32-bit lane offset inside
     // the tile (at most BN rows of the largest row stride the entry point admits); rows beyond the end of the
@@ -325,7 +357,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
         const unsigned vd = kd + (WIDE ? NB * TILEB : TILEB);
         const unsigned char* const kt = kg + (size_t)tile * BN * p.k_rs;
         const unsigned char* const vt = vg + (size_t)tile * BN * p.v_rs;
-        const int last_row = S - 1 - tile * BN;  // of this tile, counted from its first row; >= 0
+        const int last_row = Sk - 1 - tile * BN;  // of this tile, counted from its first row; >= 0
         if constexpr (ACC) {
 #pragma unroll
             for (int n = 0; n < LDW; ++n) {
@@ -396,8 +428,9 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
         for (int r = 0; r < 16; ++r)
             oacc[db][r] = 0.f;
     // running max, in the exp2 domain (already times c).  A key group may see nothing but masked keys of a row, so
-    // with several the start is finite: the lowest value there is, below any score that is itself finite.
-    float m_run = NG == 1 ? -INFINITY : -FLT_MAX;
+    // with several (and where a row may see nothing at all) the start is finite: the lowest value there is, below any score
+    // that is itself finite.
+    float m_run = NG == 1 && !PACKED ? -INFINITY : -FLT_MAX;
     float l_run = 0.f;        // this lane's share of the running sum (its 16 of every 32 keys)
     // What the sum of P as rounded for the second product, the divisor of O, has over l (this lane's share; see
     // "the two sums" in kernel 2).  It is touched only in rare blocks and in the epilogue, so it lives in a word
@@ -464,7 +497,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 
         // Causal block skipping per wavefront: nothing to do if every key of the tile lies
         // beyond this wavefront's last query.
-        const bool active = (!CAUSAL || kv0 <= q_wave0 + 31) && (NG == 1 || j < my_tiles);
+        const bool active = (!CAUSAL || kv0 <= q_wave0 + 31 + ahead) && (NG == 1 || j < my_tiles);
         if (active) {
             f32x16_t sacc[KB];
 #pragma unroll
@@ -503,14 +536,14 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
                 }
             }
             // Mask only where the tile straddles the diagonal or the end of the sequence.
-            const bool need_mask = (CAUSAL && kv0 + BN - 1 > q_wave0) || (kv0 + BN > S);
+            const bool need_mask = (CAUSAL && kv0 + BN - 1 > q_wave0 + ahead) || (kv0 + BN > Sk);
             if (need_mask) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = kv0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        const bool dead = (CAUSAL && key > my_q) || key >= S;
+                        const bool dead = (CAUSAL && key > my_q + ahead) || key >= Sk;
                         sacc[kb][r] = dead ? -INFINITY : sacc[kb][r];
                     }
             }
@@ -655,10 +688,12 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
     // Epilogue: one division by l (the per-step divide/multiply pairs telescope away), lse, store.
     const float l_tot = l_run + __shfl_xor(l_run, 32);
     const float dl_run = dl_slot();
-    const float inv_l = 1.0f / (l_tot + (dl_run + __shfl_xor(dl_run, 32)));
-    if (my_q < S && p.lse != nullptr && h == 0)
-        p.lse[(size_t)bh * S + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
-    unsigned char* const o_bh = (unsigned char*)p.o + b * p.o_bs + hq * p.o_hs;
+    float inv_l = 1.0f / (l_tot + (dl_run + __shfl_xor(dl_run, 32)));
+    if constexpr (PACKED)
+        inv_l = l_tot > 0.f ? inv_l : 0.f;  // a row that sees nothing: O = 0, and lse is -inf by itself
+    if (my_q < Sq && p.lse != nullptr && h == 0)
+        p.lse[lse_first + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+    unsigned char* const o_bh = (unsigned char*)p.o + o_first + hq * p.o_hs;
     if constexpr (DT_OUT != NAUT_F32) {
         // 16-bit O leaves through LDS in whole rows: a lane owns 4 consecutive d of one query (8 bytes, 32
         // different rows per store instruction); after the exchange D/8 lanes write one row with 16 bytes
@@ -699,11 +734,11 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 #pragma unroll
             for (int i = 0; i < BATCH; ++i) {
                 const int q = q_wave0 + (i0 + i) * RPI + ln / CPRO;
-                if (q < S && ln % CPRO < cpr)  // not the rows beyond S, not the padding columns of a narrower head
+                if (q < Sq && ln % CPRO < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
                     *(i32x4_a8*)(o_bh + (size_t)q * p.o_rs + (ln % CPRO) * 16) = rows[i];
             }
         }
-    } else if (my_q < S) {
+    } else if (my_q < Sq) {
         unsigned char* og = o_bh + (size_t)my_q * p.o_rs;
 #pragma unroll
         for (int db = 0; db < DB; ++db)

@@ -73,8 +73,9 @@ struct Pieces {
 template <int D, int QH, int NWV, int NG>
 constexpr int pipe_waves_per_simd() { return D <= 64 && QH == 1 && NG == 1 ? 3 : 2; }
 
-template <int D, int DT_IN, int DT_OUT, bool CAUSAL, int QH, int NWV, int NG = 1>
-__global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>())) void naut_fwd_kernel_pipe(const Params p)
+// PACKED: sequences back to back (naut_packed.h), Sq queries at the end of Sk keys; rows may see nothing.
+template <int D, int DT_IN, int DT_OUT, bool CAUSAL, int QH, int NWV, int NG = 1, bool PACKED = false>
+__global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>())) void naut_fwd_kernel_pipe(const ParamsOf<PACKED> p)
 {
     using T = In<DT_IN>;
     using PC = Pieces<QH>;
@@ -118,38 +119,65 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     // causal, D = 64, twelve heads to an XCD: six and six 76.2 us, all at once 65.7; 128 heads, S = 4096, D = 128 eight at a time 529,
     // sixteen 540; 256 heads, S = 640, causal, D = 64 groups 30.8, all 27.2; without the mask a group's tiles are alike, and
     // groups cost nothing).
-    const int nbh = p.B * p.Hq;
-    const int nqt = BM == BM2 ? p.nqt2 : p.nqt;
-    constexpr int PER_CU = NWV * NG == 8 ? 1 : pipe_waves_per_simd<D, QH, NWV, NG>();  // work-groups that share a CU
-    constexpr int AT_ONCE = D <= 64 ? 2 * HEADS_AT_ONCE : HEADS_AT_ONCE;               // (their K and V are half the bytes)
-    const int xcd = blockIdx.x & 7, n_xcd = (nbh * nqt - xcd + 7) >> 3;                // work-groups of this XCD
-    int qt, bh;
-    if (n_xcd <= 32 * PER_CU) {
-        int s = (int)blockIdx.x >> 3;
-        if (CAUSAL && PER_CU == 2 && s >= 32)
-            s = 31 + n_xcd - s;
-        const int bid = s * 8 + xcd;
-        qt = nqt - 1 - bid / nbh;
-        bh = bid % nbh;
-    } else {
-        const int hpx = nbh >> 3;
-        const bool all = 2 * hpx <= 3 * AT_ONCE || (CAUSAL && (long long)hpx * p.S * ROWB <= 3 << 20);
-        const QueryTile t = tile_by_head(blockIdx.x, nbh, nqt, all ? 1 : (hpx + AT_ONCE / 2) / AT_ONCE);
+    int qt, hq, Sq, Sk;
+    long long q_first, k_first, v_first, o_first, lse_first;  // bytes (lse: values) to the sequence's first row
+    if constexpr (PACKED) {
+        const PackedTile t = packed_tile<BM>(p, blockIdx.x, lane);
+        if (t.qt < 0)
+            return;
         qt = t.qt;
-        bh = t.bh;
+        hq = t.hq;
+        Sq = t.Sq;
+        Sk = t.Sk;
+        if (Sk == 0 || (CAUSAL && (qt + 1) * BM + Sk <= Sq)) {
+            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, hq, t.q0 + qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
+            return;
+        }
+        q_first = (long long)t.q0 * p.q_rs;
+        k_first = (long long)t.k0 * p.k_rs;
+        v_first = (long long)t.k0 * p.v_rs;
+        o_first = (long long)t.q0 * p.o_rs;
+        lse_first = (long long)hq * p.Tq + t.q0;
+    } else {
+        const int nbh = p.B * p.Hq;
+        const int nqt = BM == BM2 ? p.nqt2 : p.nqt;
+        constexpr int PER_CU = NWV * NG == 8 ? 1 : pipe_waves_per_simd<D, QH, NWV, NG>();  // work-groups that share a CU
+        constexpr int AT_ONCE = D <= 64 ? 2 * HEADS_AT_ONCE : HEADS_AT_ONCE;               // (their K and V are half the bytes)
+        const int xcd = blockIdx.x & 7, n_xcd = (nbh * nqt - xcd + 7) >> 3;                // work-groups of this XCD
+        int bh;
+        if (n_xcd <= 32 * PER_CU) {
+            int s = (int)blockIdx.x >> 3;
+            if (CAUSAL && PER_CU == 2 && s >= 32)
+                s = 31 + n_xcd - s;
+            const int bid = s * 8 + xcd;
+            qt = nqt - 1 - bid / nbh;
+            bh = bid % nbh;
+        } else {
+            const int hpx = nbh >> 3;
+            const bool all = 2 * hpx <= 3 * AT_ONCE || (CAUSAL && (long long)hpx * p.S * ROWB <= 3 << 20);
+            const QueryTile t = tile_by_head(blockIdx.x, nbh, nqt, all ? 1 : (hpx + AT_ONCE / 2) / AT_ONCE);
+            qt = t.qt;
+            bh = t.bh;
+        }
+        const int b = bh / p.Hq;
+        hq = bh % p.Hq;
+        Sq = Sk = p.S;
+        q_first = b * p.q_bs;
+        k_first = b * p.k_bs;
+        v_first = b * p.v_bs;
+        o_first = b * p.o_bs;
+        lse_first = (long long)bh * p.S;
     }
-    const int b = bh / p.Hq;
-    const int hq = bh % p.Hq;
+    const int ahead = PACKED ? Sk - Sq : 0;  // keys before the first query's own
     const int hk = hq / (p.Hq / p.Hkv);
-    const int S = p.S;
     const float c = p.c;
     const float p_limit = p.p_limit;
     float c_v = c;  // copy held in a vector register: an FMA with a scalar-register operand issues at the slower rate
     asm volatile("" : "+v"(c_v));
 
-    const unsigned char* qg = (const unsigned char*)p.q + b * p.q_bs + hq * p.q_hs;
-    const unsigned char* kg = (const unsigned char*)p.k + b * p.k_bs + hk * p.k_hs;
-    const unsigned char* vg = (const unsigned char*)p.v + b * p.v_bs + hk * p.v_hs;
+    const unsigned char* qg = (const unsigned char*)p.q + q_first + hq * p.q_hs;
+    const unsigned char* kg = (const unsigned char*)p.k + k_first + hk * p.k_hs;
+    const unsigned char* vg = (const unsigned char*)p.v + v_first + hk * p.v_hs;
     const int cpr = p.cpr;
 
     const int Q0 = qt * BM + wave * WQ;  // first query of this wavefront
@@ -162,7 +190,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     i32x4_t qf[QH][KS];
 #pragma unroll
     for (int hf = 0; hf < QH; ++hf) {
-        const int q_ld = qrow[hf] < S ? qrow[hf] : S - 1;
+        const int q_ld = qrow[hf] < Sq ? qrow[hf] : Sq - 1;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             // Unconditional, from a chunk that exists; the padding chunks of a narrower head are zeroed when Q is pinned
@@ -172,8 +200,10 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             qf[hf][ks] = *(const i32x4_t*)(qg + (size_t)q_ld * p.q_rs + ch * 16);
         }
     }
-    const int kv_end_wg = CAUSAL ? (S < (qt + 1) * BM ? S : (qt + 1) * BM) : S;
-    const int kv_end_w = Q0 >= S ? 0 : (CAUSAL ? (S < Q0 + WQ ? S : Q0 + WQ) : S);
+    const int kv_end_wg = CAUSAL ? (Sk < (qt + 1) * BM + ahead ? Sk : (qt + 1) * BM + ahead) : Sk;
+    int kv_end_w = Q0 >= Sq ? 0 : (CAUSAL ? (Sk < Q0 + WQ + ahead ? Sk : Q0 + WQ + ahead) : Sk);
+    if constexpr (PACKED)
+        kv_end_w = kv_end_w > 0 ? kv_end_w : 0;
     const int ntiles = (kv_end_wg + BN - 1) / BN;
     // tiles and blocks below count those of a key group: grp, grp + NG, ...
     auto of_group = [&](int n) { return n > grp ? (n - grp + NG - 1) / NG : 0; };
@@ -210,7 +240,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         t.rsrc.y = __builtin_amdgcn_readfirstlane((int)(a >> 32) & 0xffff);
         t.rsrc.w = 0x00020000;
         t.off = (unsigned)(grp < ntiles ? grp : ntiles - 1) * (unsigned)(BN * rs);
-        t.range64 = (uint64_t)(S - 1) * (unsigned)rs + (unsigned)(cpr * 16);
+        t.range64 = (uint64_t)(Sk - 1) * (unsigned)rs + (unsigned)(cpr * 16);
         // the group's last tile (a group without one: a tile that exists, for nobody)
         t.end64 = (uint64_t)(grp < ntiles ? ntiles - 1 - (ntiles - 1 - grp) % NG : ntiles - 1) * (unsigned)(BN * rs);
         t.rsrc.z = __builtin_amdgcn_readfirstlane((int)(unsigned)(t.range64 >> 32 ? 0xffffffffu : t.range64));
@@ -284,12 +314,13 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             const int key = key0 + 8 * (r >> 2) + (r & 3);
 #pragma unroll
             for (int hf = 0; hf < QH; ++hf)
-                s_[hf][r] = (key >= kv_end_w || (CAUSAL && key > qrow[hf])) ? -INFINITY : s_[hf][r];
+                s_[hf][r] = (key >= kv_end_w || (CAUSAL && key > qrow[hf] + ahead)) ? -INFINITY : s_[hf][r];
         }
     };
-    // first block that needs masking: 32k+31 > Q0 (causal; Q0 is a multiple of 32) or 32k+32 > kv_end_w
+    // first block that needs masking: 32k+31 > Q0 + ahead (causal; Q0 is a multiple of 32) or 32k+32 > kv_end_w
     const int kc2 = kv_end_w / BN;
-    const int k_mask_from = of_group(CAUSAL ? (Q0 / BN < kc2 ? Q0 / BN : kc2) : kc2);
+    const int kc1 = !PACKED ? Q0 / BN : Q0 + ahead < 0 ? 0 : (Q0 + ahead + 1) / BN;
+    const int k_mask_from = of_group(CAUSAL ? (kc1 < kc2 ? kc1 : kc2) : kc2);
     // max of three; the device code is compiled with NaNs assumed absent, so this is one v_max3_f32 with no quieting of
     // the operands
     auto max3 = [](float x, float y, float z) { return __builtin_fmaxf(__builtin_fmaxf(x, y), z); };
@@ -663,7 +694,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         __syncthreads();
         if (grp > 0)
             return;
-        // The halves of a row hold the same maximum, and key 0, which every row sees, is the first group's.
+        // The halves of a row hold the same maximum, and key 0, which every row that sees a key sees, is the first group's.
         const float m_new = __builtin_fmaxf(m_run[0], ml[0]);
         const float f0 = __builtin_amdgcn_exp2f(m_run[0] - m_new), f1 = __builtin_amdgcn_exp2f(ml[0] - m_new);
         m_run[0] = m_new;
@@ -680,10 +711,10 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             }
     }
     // ---- epilogue ----
-    if (Q0 >= S)
+    if (Q0 >= Sq)
         return;
     constexpr int OUTB = DT_OUT == NAUT_F32 ? 4 : 2;
-    unsigned char* const o_bh = (unsigned char*)p.o + b * p.o_bs + hq * p.o_hs;
+    unsigned char* const o_bh = (unsigned char*)p.o + o_first + hq * p.o_hs;
     // 16-bit O leaves through LDS in whole rows: a lane owns 4 consecutive d of one query (8 bytes, 32 different rows per
     // store instruction); after the exchange 16 lanes (D = 128) write one 256-byte row with 16 bytes each.
     constexpr int CPRO = W / 8, R256 = ROWB >= 256 ? 1 : 256 / ROWB;  // 16-byte chunks per row, rows per 256-byte bank line
@@ -696,10 +727,12 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     for (int hf = 0; hf < QH; ++hf) {
         const int q = qrow[hf];
         const float lt = 4.0f * half_sum(lq_run[hf]);
-        const float inv_l = 1.0f / (lt + half_sum(dl_run[hf]));  // rows beyond S: never stored
-        if (p.lse != nullptr && h == 0 && q < S)
-            p.lse[(size_t)bh * S + q] = (m_run[hf] + __builtin_amdgcn_logf(lt)) * 0.6931471805599453f;
-        unsigned char* const og = o_bh + (size_t)(q < S ? q : 0) * p.o_rs;
+        float inv_l = 1.0f / (lt + half_sum(dl_run[hf]));  // rows beyond Sq: never stored
+        if constexpr (PACKED)
+            inv_l = lt > 0.f ? inv_l : 0.f;  // a row that sees nothing: O = 0, and lse is -inf by itself
+        if (p.lse != nullptr && h == 0 && q < Sq)
+            p.lse[lse_first + q] = (m_run[hf] + __builtin_amdgcn_logf(lt)) * 0.6931471805599453f;
+        unsigned char* const og = o_bh + (size_t)(q < Sq ? q : 0) * p.o_rs;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -710,7 +743,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
                 if constexpr (OUTB == 2)
                     *(i32x2_t*)(staged(32 * hf + l32, d >> 3) + (d & 7) * 2) =
                         i32x2_t{In<DT_OUT>::pack2(x.x, x.y), In<DT_OUT>::pack2(x.z, x.w)};
-                else if (q < S && d < cpr * 8)  // not the padding columns of a narrower head dimension
+                else if (q < Sq && d < cpr * 8)  // not the padding columns of a narrower head dimension
                     *(f32x4_t*)(og + d * 4) = x;
             }
     }
@@ -728,7 +761,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         for (int i = 0; i < WQ / RPI; ++i) {
             const int ch = lane % CPRO;
             const int q = Q0 + i * RPI + lane / CPRO;
-            if (q < S && ch < cpr)  // not the rows beyond S, not the padding columns of a narrower head
+            if (q < Sq && ch < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
                 *(i32x4_a8*)(o_bh + (size_t)q * p.o_rs + ch * 16) = rows[i];
         }
     }

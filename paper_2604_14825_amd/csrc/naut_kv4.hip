@@ -1,0 +1,874 @@
+// naut_kv4.hip -- a key/value cache in 4 bits for gfx950 (MI355X): rows into it, rows out of it, decode-time attention over it.
+//
+// The format is OCP MXFP4: blocks of 32 values, E2M1 codes under one power of two.  gfx950 converts between such codes and
+// 16-bit values with the block's power in one instruction per pair, and a code times its power is exact in bf16, so the
+// attention runs on the cache's values as they are, on the 16-bit matrix instructions.
+#include <hip/hip_runtime.h>
+
+#include <cfloat>
+#include <cmath>
+#include <cstdint>
+#include <cstdio>
+
+#include "naut_attn.h"
+#include "naut_common.h"
+
+namespace {
+
+using namespace naut;
+
+constexpr int MX = 32;  // values per block
+
+// The value of a scale byte as the conversions take it (its exponent field).
+__device__ __forceinline__ float mx_scale(int byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Pairs of values: code byte I of `word` times `scale`, and back.
+template <int DT>
+struct Mx;
+template <>
+struct Mx<NAUT_BF16> {
+    typedef bf16x2_t pair;
+    static constexpr int MOST = 252;  // 6 * 2^125 is finite, 4 * 2^126 is not
+    template <int I>
+    static __device__ __forceinline__ int decode(int word, float scale)
+    {
+        return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((unsigned)word, scale, I));
+    }
+    template <int I>
+    static __device__ __forceinline__ int encode(int old, int two, float scale)
+    {
+        return (int)__builtin_amdgcn_cvt_scalef32_pk_fp4_bf16((unsigned)old, __builtin_bit_cast(pair, two), scale, I);
+    }
+    static __device__ __forceinline__ float high(int two) { return __builtin_bit_cast(float, two & (int)0xffff0000); }
+    static __device__ __forceinline__ float low(int two) { return __builtin_bit_cast(float, two << 16); }
+    static __device__ __forceinline__ int scale_of(int byte) { return byte; }
+    static __device__ __forceinline__ f32x4_t mfma(i32x4_t a, i32x4_t b, f32x4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+    }
+};
+template <>
+struct Mx<NAUT_F16> {
+    typedef f16x2_t pair;
+    static constexpr int MOST = 140;  // 6 * 2^13 = 49152
+    template <int I>
+    static __device__ __forceinline__ int decode(int word, float scale)
+    {
+        return __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((unsigned)word, scale, I));
+    }
+    template <int I>
+    static __device__ __forceinline__ int encode(int old, int two, float scale)
+    {
+        return (int)__builtin_amdgcn_cvt_scalef32_pk_fp4_f16((unsigned)old, __builtin_bit_cast(pair, two), scale, I);
+    }
+    static __device__ __forceinline__ float high(int two) { return (float)__builtin_bit_cast(pair, two).y; }
+    static __device__ __forceinline__ float low(int two) { return (float)__builtin_bit_cast(pair, two).x; }
+    static __device__ __forceinline__ int scale_of(int byte) { return byte < MOST ? byte : MOST; }  // no value becomes infinite
+    static __device__ __forceinline__ f32x4_t mfma(i32x4_t a, i32x4_t b, f32x4_t c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+    }
+};
+
+// ---- rows into and out of the cache ----------------------------------------------------------------------------------
+
+struct RowParams {
+    unsigned char *codes[2], *scales[2];  // K, V
+    unsigned char* rows[2];               // 16-bit rows
+    long long hs[2], rs[2];               // their head and row strides, in bytes
+    const int* slots;
+    long long c_b, c_h, c_s, s_b, s_h, s_s;
+    int T, B, Hkv, S;
+    int oct;                              // eights of values per row
+};
+
+// A thread takes eight values, four neighbours a block: 16 bytes of a row, 4 bytes of codes, so that both sides of a wavefront
+// are contiguous.  Bound by memory.
+struct RowPlace {
+    unsigned char *codes, *scale, *row;
+    bool ok;
+};
+__device__ __forceinline__ RowPlace row_place(const RowParams& p, int kv, int x)
+{
+    const int o = x % p.oct, th = x / p.oct, hd = th % p.Hkv, t = th / p.Hkv;
+    RowPlace r;
+    const int slot = t < p.T ? p.slots[t] : -1;
+    r.ok = slot >= 0 && (unsigned)slot < (unsigned)p.B * (unsigned)p.S;
+    const int b = slot / p.S, s = slot % p.S;  // not used unless ok
+    r.codes = p.codes[kv] + b * p.c_b + hd * p.c_h + s * p.c_s + o * 4;
+    r.scale = p.scales[kv] + b * p.s_b + hd * p.s_h + s * p.s_s + (o >> 2);
+    r.row = p.rows[kv] + t * p.rs[kv] + hd * p.hs[kv] + o * 16;
+    return r;
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void naut_kv4_store_kernel(const RowParams p)
+{
+    using X = Mx<DT>;
+    const RowPlace r = row_place(p, blockIdx.y, blockIdx.x * 256 + threadIdx.x);
+    i32x4_t w = {0, 0, 0, 0};
+    if (r.ok)
+        w = *(const i32x4_t*)r.row;
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        a = fmaxf(a, fmaxf(fabsf(X::low(w[i])), fabsf(X::high(w[i]))));
+    // the largest of the block: four neighbouring lanes have its values (D is a multiple of 32)
+    a = fmaxf(a, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a), 0xb1, 0xf, 0xf, true)));  // lane ^ 1
+    a = fmaxf(a, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, a), 0x4e, 0xf, 0xf, true)));  // lane ^ 2
+    // a = m 2^e, 1 <= m < 2: the power is e - 2, one more from m = 1.75 on, where a quarter carries into the exponent
+    int byte = ((__builtin_bit_cast(int, a) + 0x00200000) >> 23) - 2;
+    byte = byte < 1 ? 1 : byte < X::MOST ? byte : X::MOST;
+    const float scale = mx_scale(byte);
+    int codes = X::template encode<0>(0, w[0], scale);
+    codes = X::template encode<1>(codes, w[1], scale);
+    codes = X::template encode<2>(codes, w[2], scale);
+    codes = X::template encode<3>(codes, w[3], scale);
+    if (r.ok) {
+        *(int*)r.codes = codes;
+        if ((threadIdx.x & 3) == 0)
+            *r.scale = (unsigned char)byte;
+    }
+}
+
+template <int DT>
+__global__ __launch_bounds__(256) void naut_kv4_load_kernel(const RowParams p)
+{
+    using X = Mx<DT>;
+    const RowPlace r = row_place(p, blockIdx.y, blockIdx.x * 256 + threadIdx.x);
+    if (!r.ok)
+        return;
+    const int codes = *(const int*)r.codes;
+    const float scale = mx_scale(X::scale_of(*r.scale));
+    *(i32x4_t*)r.row = i32x4_t{X::template decode<0>(codes, scale), X::template decode<1>(codes, scale),
+                               X::template decode<2>(codes, scale), X::template decode<3>(codes, scale)};
+}
+
+int check_cache(const naut_kv4_cache* c)
+{
+    if (!c || !c->k_codes || !c->k_scales || !c->v_codes || !c->v_scales)
+        return fail(NAUT_ERR_NULL, "the cache and its four pointers must be non-NULL");
+    if (c->B <= 0 || c->Hkv <= 0 || c->S <= 0 || c->D <= 0)
+        return fail(NAUT_ERR_SHAPE, "the cache's B, Hkv, S and D must be positive");
+    if (c->D % MX != 0 || c->D > 256)
+        return fail(NAUT_ERR_UNSUPPORTED, "the cache's D must be a multiple of 32, at most 256");
+    if ((long long)c->B * c->S > 0x7fffffffLL)
+        return fail(NAUT_ERR_UNSUPPORTED, "the cache's B*S exceeds 2^31 - 1");
+    if (((uintptr_t)c->k_codes | (uintptr_t)c->v_codes) & 15u || c->c_b < 0 || c->c_h < 0 || (c->c_b | c->c_h | c->c_s) % 16 != 0)
+        return fail(NAUT_ERR_ALIGN, "codes must be 16-byte aligned, their strides non-negative multiples of 16 bytes");
+    const int row = naut_kv4_scale_bytes(c->D);
+    if (((uintptr_t)c->k_scales | (uintptr_t)c->v_scales) % row != 0 || c->s_b < 0 || c->s_h < 0 || (c->s_b | c->s_h | c->s_s) % row != 0)
+        return fail(NAUT_ERR_ALIGN, "scales and their strides must be aligned to naut_kv4_scale_bytes(), the strides non-negative");
+    if (c->c_s < c->D / 2 || c->s_s < row)
+        return fail(NAUT_ERR_SHAPE, "a position's stride is smaller than its row: rows would overlap");
+    if (c->c_s > 1LL << 23 || c->s_s > 1LL << 23)
+        return fail(NAUT_ERR_UNSUPPORTED, "position stride too large");
+    return NAUT_OK;
+}
+
+// Arguments of a store (writes the cache) or a load (writes the rows).
+int rows_of(const void* k, const void* v, const naut_kv4_cache* c, const int* slots, int T, int dtype, const naut_strides* st,
+            bool load, RowParams* p)
+{
+    const int rc = check_cache(c);
+    if (rc != NAUT_OK)
+        return rc;
+    if (T < 0)
+        return fail(NAUT_ERR_SHAPE, "T must not be negative");
+    if (T > 0 && (!k || !v || !slots))
+        return fail(NAUT_ERR_NULL, "k, v and slots must be non-NULL device pointers");
+    if (dtype != NAUT_BF16 && dtype != NAUT_F16)
+        return fail(NAUT_ERR_UNSUPPORTED, "k and v must be bf16 or f16");
+    if (((uintptr_t)k | (uintptr_t)v) & 15u)
+        return fail(NAUT_ERR_ALIGN, "k and v must be 16-byte aligned");
+    if ((uintptr_t)slots & 3u)
+        return fail(NAUT_ERR_ALIGN, "slots must be 4-byte aligned");
+    naut_strides cs = {};
+    cs.k_h = cs.v_h = c->D;
+    cs.k_s = cs.v_s = (long long)c->Hkv * c->D;
+    if (!st)
+        st = &cs;
+    const long long strides[4] = {st->k_h, st->k_s, st->v_h, st->v_s};
+    for (long long x : strides)
+        if (x < 0 || x % 8 != 0 || (load && x == 0))
+            return fail(NAUT_ERR_ALIGN, "k/v strides must be multiples of 8 elements (16 bytes), not negative (load: positive)");
+    // a store needs every row's bytes to itself
+    if (!load && ((c->Hkv > 1 && (c->c_h == 0 || c->s_h == 0)) || (c->B > 1 && (c->c_b == 0 || c->s_b == 0))))
+        return fail(NAUT_ERR_SHAPE, "a cache that is stored to cannot have heads or sequences in the same place (stride 0)");
+    if (load && (st->k_s < c->D || st->v_s < c->D))
+        return fail(NAUT_ERR_SHAPE, "a sequence stride is smaller than D: rows would overlap");
+    if ((long long)T * c->Hkv * (c->D / 8) > 0x7fffffffLL - 255)
+        return fail(NAUT_ERR_UNSUPPORTED, "too many rows for one call");
+    p->codes[0] = (unsigned char*)c->k_codes;
+    p->codes[1] = (unsigned char*)c->v_codes;
+    p->scales[0] = (unsigned char*)c->k_scales;
+    p->scales[1] = (unsigned char*)c->v_scales;
+    p->rows[0] = (unsigned char*)k;
+    p->rows[1] = (unsigned char*)v;
+    p->hs[0] = st->k_h * 2;
+    p->hs[1] = st->v_h * 2;
+    p->rs[0] = st->k_s * 2;
+    p->rs[1] = st->v_s * 2;
+    p->slots = slots;
+    p->c_b = c->c_b;
+    p->c_h = c->c_h;
+    p->c_s = c->c_s;
+    p->s_b = c->s_b;
+    p->s_h = c->s_h;
+    p->s_s = c->s_s;
+    p->T = T;
+    p->B = c->B;
+    p->Hkv = c->Hkv;
+    p->S = c->S;
+    p->oct = c->D / 8;
+    return NAUT_OK;
+}
+
+int launched()
+{
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? fail_launch(e) : NAUT_OK;
+}
+
+// ---- decode-time attention over the cache ----------------------------------------------------------------------------
+//
+// Bound by reading the cache once: 2 (D/2 + D/32) bytes a key and K/V head.  A wavefront takes blocks of 32 keys, in two key
+// tiles of 16, against tiles of 16 query rows (the R = Hq/Hkv * Sq rows that share a K/V head): S^T = K Q^T and O^T += V^T P^T
+// on the 16x16x32 matrix instructions, the softmax in between as in the 16-bit kernels, lane-local but for the sum and the
+// maximum over the four lane groups of 16.
+//   K goes from memory into registers: a lane's 16 bytes of codes are one block of 32 values of one key, four conversions make
+// eight of them an A operand, and Q is loaded in the order that this gives the contraction.  V's codes come in the same
+// way, are converted, and pass through the wavefront's own LDS as 16-bit rows to be read transposed.
+constexpr int KV_BLK = 32;    // keys per block
+constexpr int KV_WAVES = 4;   // wavefronts of a split kernel
+constexpr int KV_TARGET = 1024;  // work-groups that the plan aims at: four to a CU
+constexpr int MRG_WAVES = 4;
+
+struct Kv4Params {
+    const void* q;
+    void* o;
+    float* lse;
+    const unsigned char *codes[2], *scales[2];  // K, V
+    long long c_b, c_h, c_s, s_b, s_h, s_s;
+    const int* lens;
+    float* ws;        // partial O [nparts][rows][D], then m [nparts][rows], l [nparts][rows], then {first split, splits} [B]
+    int B, Hq, Hkv, Sq, S;
+    int R;            // query rows per (sequence, K/V head)
+    int rows;         // of a chunk of them, a multiple of 16
+    int nchunks;
+    int P;            // splits of all sequences together, at most (the grid)
+    int least;        // blocks per split, at least
+    int causal;
+    float c;          // scale * log2(e), > 0
+    int out_f32;
+    long long q_bs, q_hs, o_bs, o_hs;
+    int q_rs, o_rs;
+    int nb;           // blocks of 32 values in a row = D / 32
+};
+
+__device__ __forceinline__ int kv4_len(const Kv4Params& p, int b)
+{
+    const int n = p.lens ? p.lens[b] : p.S;
+    return n < 0 ? 0 : n < p.S ? n : p.S;
+}
+
+// ceil(x / y) for 0 <= x < 2^26, y > 0: by the reciprocal, and put right
+__device__ __forceinline__ int ceil_div(int x, int y, float rcp)
+{
+    int q = (int)((float)x * rcp);
+    int r = x - q * y;
+    q += r > 0;
+    r -= r > 0 ? y : 0;
+    q += r > 0;
+    r -= r > 0 ? y : 0;
+    return q - (r <= -y);
+}
+
+struct Kv4Split {
+    int b, split, nsplit, first;  // sequence, its split, its splits, the index of its first split
+    int len, begin, end;          // keys, blocks
+};
+
+// Which part of which sequence split x is: every sequence is cut into equal parts of at most L blocks (an empty one is one
+// part), L the least at which the parts are no more than P, found by halving between the mean and twice the longest.  64
+// sequences at a time, one to a lane.
+__device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, Kv4Split* out)
+{
+    const int nch = (p.B + 63) >> 6;
+    auto blocks = [&](int c) { return c * 64 + lane < p.B ? (kv4_len(p, c * 64 + lane) + KV_BLK - 1) / KV_BLK : -1; };
+    const int mine = blocks(0);  // the first chunk's, kept
+    auto of = [&](int c) { return c == 0 ? mine : blocks(c); };
+    auto parts = [&](int n, int L, float rcp) { return n < 0 ? 0 : n == 0 ? 1 : ceil_div(n, L, rcp); };
+    auto count = [&](int L) {
+        const float rcp = __builtin_amdgcn_rcpf((float)L);
+        int sum = 0;
+        for (int c = 0; c < nch; ++c)
+            sum += parts(of(c), L, rcp);
+        return wave_sum(sum);
+    };
+    int total = 0;  // blocks, rounded up: in units that do not overflow
+    for (int c = 0; c < nch; ++c)
+        total += of(c) > 0 ? of(c) : 0;
+    total = wave_sum(total);
+    int lo = (total + p.P - 1) / p.P;
+    lo = lo > p.least ? lo : p.least;
+    if (count(lo) > p.P) {
+        int hi = (p.S + KV_BLK - 1) / KV_BLK;  // one part each: B <= P
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (count(mid) <= p.P)
+                hi = mid;
+            else
+                lo = mid + 1;
+        }
+    }
+    const float rcp = __builtin_amdgcn_rcpf((float)lo);
+    int before = 0;
+    for (int c = 0; c < nch; ++c) {
+        const int n = of(c), m = parts(n, lo, rcp);
+        const int incl = wave_scan(m) + before;
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > x);
+        if (mask == 0) {
+            before = __builtin_amdgcn_readlane(incl, 63);
+            continue;
+        }
+        const int src = __builtin_ctzll(mask);
+        out->b = c * 64 + src;
+        out->nsplit = __builtin_amdgcn_readlane(m, src);
+        out->first = __builtin_amdgcn_readlane(incl, src) - out->nsplit;
+        out->split = x - out->first;
+        const int all = __builtin_amdgcn_readlane(n, src);
+        const int each = (all + out->nsplit - 1) / out->nsplit;
+        out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, out->b));
+        out->begin = out->split * each < all ? out->split * each : all;
+        out->end = out->begin + each < all ? out->begin + each : all;
+        return true;
+    }
+    return false;
+}
+
+// A row of O (four values at d) and, from one thread, of lse: row r of (sequence b, K/V head hk).
+template <int DT>
+__device__ __forceinline__ void kv4_store_o(const Kv4Params& p, int b, int hk, int r, int d, f32x4_t o)
+{
+    const int head = hk * (p.Hq / p.Hkv) + r / p.Sq, pos = r % p.Sq;
+    unsigned char* const row = (unsigned char*)p.o + b * p.o_bs + head * p.o_hs + (long long)pos * p.o_rs;
+    if (d >= p.nb * MX)
+        return;  // padding columns of a narrower head
+    if (p.out_f32)
+        *(f32x4_t*)(row + d * 4) = o;
+    else
+        *(i32x2_t*)(row + d * 2) = i32x2_t{In<DT>::pack2(o.x, o.y), In<DT>::pack2(o.z, o.w)};
+}
+__device__ __forceinline__ void kv4_store_lse(const Kv4Params& p, int b, int hk, int r, float m, float l)
+{
+    if (p.lse != nullptr)  // log2(0) = -inf: a row that saw nothing
+        p.lse[((size_t)b * p.Hkv + hk) * p.R + r] = (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
+// maximum and sum over the four lane groups of 16
+__device__ __forceinline__ float group_max(float x)
+{
+    float a = x, b = x;
+    asm volatile(NAUT_NOP_SHORT "v_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return half_max(fmaxf(a, b));
+}
+__device__ __forceinline__ float group_sum(float x)
+{
+    float a = x, b = x;
+    asm volatile(NAUT_NOP_SHORT "v_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    a += b;
+    b = a;
+    asm volatile(NAUT_NOP_SHORT "v_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return a + b;
+}
+
+// Byte offset of 16-byte chunk c of V's row r (D 16-bit values) in LDS.  A transposed read takes 32 bytes of each of 16 rows, a
+// write 16 bytes of each of eight: pairs of chunks are XOR-ed with the row so that both go to different banks.
+template <int D>
+__device__ __forceinline__ int v4_off(int r, int c)
+{
+    const int key = D == 64 ? (r >> 1) & 3 : r & 7;
+    return r * (D * 2) + ((c ^ (key << 1)) << 4);
+}
+
+template <int D, int DT, int RT>
+__global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv4Params p)
+{
+    using X = Mx<DT>;
+    constexpr int NW = KV_WAVES;
+    constexpr int KS = D / 32;             // words of codes, and MFMAs, per key tile
+    constexpr int DT16 = D / 16;           // 16-row tiles of O^T
+    constexpr int VB = KV_BLK * D * 2;     // a block of V in LDS
+    constexpr int OB = RT * 16 * D * 4;    // a wavefront's O
+    constexpr int REGION = VB > OB ? VB : OB;
+    __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * REGION];
+    __shared__ float ml_lds[NW][2][RT * 16];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g4 = lane >> 4;
+    const int chunk = blockIdx.y, hk = blockIdx.z;
+    Kv4Split sp;
+    if (!kv4_split(p, blockIdx.x, lane, &sp))
+        return;
+    const int b = sp.b, len = sp.len;
+    const int g = p.Hq / p.Hkv;
+    const int row0 = chunk * p.rows;
+    const float c = p.c;
+    const unsigned char* const cg[2] = {p.codes[0] + b * p.c_b + hk * p.c_h, p.codes[1] + b * p.c_b + hk * p.c_h};
+    const unsigned char* const sg[2] = {p.scales[0] + b * p.s_b + hk * p.s_h, p.scales[1] + b * p.s_b + hk * p.s_h};
+
+    // A lane's words of a key's row: word ks holds the values dim(ks) .. + 8, which is the contraction order of MFMA ks.
+    auto dim = [&](int ks) { return D == 64 ? 16 * g4 + 8 * ks : 32 * (4 * (ks >> 2) + g4) + 8 * (ks & 3); };
+    // the block of a lane's chunk j (D = 256 has two), a real one also where the head is narrower
+    auto blk_of = [&](int j) {
+        const int x = D == 64 ? g4 >> 1 : 4 * j + g4;
+        return x < p.nb ? x : p.nb - 1;
+    };
+    constexpr int CH = D == 256 ? 2 : 1;   // chunks per lane and key
+
+    i32x4_t qf[RT][KS];
+    int lim[RT];  // last key that the lane's row sees
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int row = row0 + rt * 16 + l16, r = row < p.R ? row : p.R - 1;
+        const unsigned char* const qr = (const unsigned char*)p.q + b * p.q_bs + (hk * g + r / p.Sq) * p.q_hs + (long long)(r % p.Sq) * p.q_rs;
+        lim[rt] = p.causal ? len - p.Sq + r % p.Sq : len - 1;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            qf[rt][ks] = dim(ks) < p.nb * MX ? *(const i32x4_t*)(qr + dim(ks) * 2) : i32x4_t{0, 0, 0, 0};
+    }
+
+    struct Block {
+        int w[2][2][KS];   // [K, V][key tile][word]
+        int s[2][2][CH];   // scale bytes
+    };
+    auto load = [&](Block& x, int blk) {
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                int key = blk * KV_BLK + t * 16 + l16;
+                key = key < len ? key : len - 1;  // the ragged last block reads its last key again
+                const unsigned char* const cr = cg[kv] + key * p.c_s;
+                const unsigned char* const sr = sg[kv] + key * p.s_s;
+                if constexpr (D == 64) {
+                    const int at = g4 * 8 < p.nb * 16 ? g4 * 8 : 0;
+                    const i32x2_t y = *(const i32x2_t*)(cr + at);
+                    x.w[kv][t][0] = y.x;
+                    x.w[kv][t][1] = y.y;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < CH; ++j) {
+                        const i32x4_t y = *(const i32x4_t*)(cr + blk_of(j) * 16);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            x.w[kv][t][4 * j + i] = y[i];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < CH; ++j)
+                    x.s[kv][t][j] = sr[blk_of(j)];
+            }
+    };
+    // eight values of word ks
+    auto values = [&](const Block& x, int kv, int t, int ks) -> i32x4_t {
+        const float s = mx_scale(X::scale_of(x.s[kv][t][CH == 1 ? 0 : ks >> 2]));
+        const int w = x.w[kv][t][ks];
+        return i32x4_t{X::template decode<0>(w, s), X::template decode<1>(w, s), X::template decode<2>(w, s), X::template decode<3>(w, s)};
+    };
+
+    unsigned char* const my = smem + wave * REGION;
+    f32x4_t oacc[RT][DT16];
+    float m_run[RT], l_run[RT];  // reference maximum (log2 units, the lowest value there is at first), the lane's share of the sum
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int dt = 0; dt < DT16; ++dt)
+            oacc[rt][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        m_run[rt] = -FLT_MAX;
+        l_run[rt] = 0.f;
+    }
+
+    for (int blk = sp.begin + wave; blk < sp.end; blk += NW) {
+        Block x;
+        load(x, blk);
+        f32x4_t s[RT][2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                s[rt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const i32x4_t kf = values(x, 0, t, ks);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+                    s[rt][t] = X::mfma(kf, qf[rt][ks], s[rt][t]);
+            }
+        }
+        // V to LDS, as rows of 16-bit values
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                *(i32x4_t*)(my + v4_off<D>(t * 16 + l16, dim(ks) >> 3)) = values(x, 1, t, ks);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        const int key0 = blk * KV_BLK;
+        i32x4_t pb[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            if (key0 + KV_BLK - 1 > len - p.Sq || key0 + KV_BLK > len) {  // some row's limit may fall inside the block
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        s[rt][t][r] = key0 + 16 * t + 4 * g4 + r > lim[rt] ? -INFINITY : s[rt][t][r];
+            }
+            float mx = s[rt][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i)
+                mx = fmaxf(mx, s[rt][i >> 2][i & 3]);
+            if (__builtin_amdgcn_ballot_w64(mx * c > m_run[rt]) != 0) {  // the largest P of a row stays exactly 1
+                const float m_new = fmaxf(m_run[rt], group_max(mx) * c);
+                const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m_new);
+                m_run[rt] = m_new;
+                l_run[rt] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT16; ++dt)
+                    oacc[rt][dt] *= alpha;
+            }
+            float e[8], sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[rt][i >> 2][i & 3], c, -m_run[rt]));
+                sum += e[i];
+            }
+            l_run[rt] += sum;
+            pb[rt] = i32x4_t{In<DT>::pack2(e[0], e[1]), In<DT>::pack2(e[2], e[3]), In<DT>::pack2(e[4], e[5]), In<DT>::pack2(e[6], e[7])};
+        }
+        // A lane's eight keys of P are 4 g4 + {0..3} of either key tile: so are those of the V^T fragments.
+#pragma unroll
+        for (int dt = 0; dt < DT16; ++dt) {
+            const int r = 4 * g4 + (l16 >> 2), d = 16 * dt + 4 * (l16 & 3);
+            const unsigned char* const a = my + v4_off<D>(r, d >> 3) + (d & 7) * 2;
+            const i16x4_t r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(a));
+            const i16x4_t r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(a + 16 * D * 2));
+            const i32x2_t lo = __builtin_bit_cast(i32x2_t, r0), hi = __builtin_bit_cast(i32x2_t, r1);
+            const i32x4_t vf = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                oacc[rt][dt] = X::mfma(vf, pb[rt], oacc[rt][dt]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");  // the next block's writes stay behind these reads
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+
+    // ---- the wavefronts' partials, merged through LDS (each in its own, now idle, region) ----
+    constexpr int Q4 = D / 4;
+    auto piece = [&](int w, int r, int q4) { return (f32x4_t*)(smem + w * REGION) + r * Q4 + (q4 ^ (r & 7)); };
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int dt = 0; dt < DT16; ++dt)
+            *piece(wave, rt * 16 + l16, 4 * dt + g4) = oacc[rt][dt];
+        const float l = group_sum(l_run[rt]);
+        if (g4 == 0) {
+            ml_lds[wave][0][rt * 16 + l16] = m_run[rt];
+            ml_lds[wave][1][rt * 16 + l16] = l;
+        }
+    }
+    __syncthreads();
+    const int rows = p.R - row0 < p.rows ? p.R - row0 : p.rows;
+    const int part = (hk * p.nchunks + chunk) * p.P + blockIdx.x;
+    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
+    float* const ws_m = p.ws + nparts * p.rows * D;
+    float* const ws_l = ws_m + nparts * p.rows;
+    if (sp.split == 0 && chunk == 0 && hk == 0 && tid == 0 && p.P > p.B) {  // for the merge
+        int* const at = (int*)(ws_l + nparts * p.rows) + 2 * b;
+        at[0] = sp.first;
+        at[1] = sp.nsplit;
+    }
+    for (int x = tid; x < rows * Q4; x += NW * 64) {
+        const int r = x / Q4, q4 = x % Q4;
+        float m = -FLT_MAX, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+            m = fmaxf(m, ml_lds[w][0][r]);
+        f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float f = __builtin_amdgcn_exp2f(ml_lds[w][0][r] - m);
+            l += f * ml_lds[w][1][r];
+            acc += *piece(w, r, q4) * f;
+        }
+        if (sp.nsplit == 1) {
+            kv4_store_o<DT>(p, b, hk, row0 + r, 4 * q4, acc * (l > 0.f ? 1.0f / l : 0.f));
+            if (q4 == 0)
+                kv4_store_lse(p, b, hk, row0 + r, m, l);
+        } else {
+            *(f32x4_t*)(p.ws + ((size_t)part * p.rows + r) * D + 4 * q4) = acc;
+            if (q4 == 0) {
+                ws_m[(size_t)part * p.rows + r] = m;
+                ws_l[(size_t)part * p.rows + r] = l;
+            }
+        }
+    }
+}
+
+// One work-group per query row: the splits of its sequence, where there are several.  Wavefront w takes splits w, w + 4, ..., eight
+// of them at a time; lanes run over D.
+template <int D, int DT>
+__global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(const Kv4Params p)
+{
+    constexpr int EPT = D / 64, BATCH = 8;
+    typedef float fe_t __attribute__((ext_vector_type(EPT)));
+    __shared__ float red_m[MRG_WAVES], red_l[MRG_WAVES];
+    __shared__ __attribute__((aligned(16))) float red_o[MRG_WAVES][D];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const int chunk = row / p.rows, r = row % p.rows;
+    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
+    const float* ws_m = p.ws + nparts * p.rows * D;
+    const float* ws_l = ws_m + nparts * p.rows;
+    const int* const at = (const int*)(ws_l + nparts * p.rows) + 2 * b;
+    const int first = at[0], nsplit = at[1];
+    if (nsplit <= 1)
+        return;  // stored already
+    const size_t part0 = (size_t)(hk * p.nchunks + chunk) * p.P + first;
+    ws_m += part0 * p.rows + r;
+    ws_l += part0 * p.rows + r;
+    const float* const ws_o = p.ws + (part0 * p.rows + r) * D;
+    fe_t acc = (fe_t)(0.f);
+    float M = -FLT_MAX, L = 0.f;
+    for (int s0 = wave; s0 < nsplit; s0 += MRG_WAVES * BATCH) {
+        float m[BATCH], l[BATCH];
+        fe_t x[BATCH];
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const int s = s0 + u * MRG_WAVES;
+            const size_t sc = s < nsplit ? s : s0;  // past the end: repeats a split, not added
+            m[u] = ws_m[sc * p.rows];
+            l[u] = ws_l[sc * p.rows];
+            x[u] = *(const fe_t*)(ws_o + sc * p.rows * D + lane * EPT);
+        }
+        float m_new = M;
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u)
+            m_new = fmaxf(m_new, m[u]);
+        const float alpha = __builtin_amdgcn_exp2f(M - m_new);
+        M = m_new;
+        L *= alpha;
+        acc *= alpha;
+#pragma unroll
+        for (int u = 0; u < BATCH; ++u) {
+            const float f = s0 + u * MRG_WAVES < nsplit ? __builtin_amdgcn_exp2f(m[u] - M) : 0.f;
+            L += f * l[u];
+            acc += f * x[u];
+        }
+    }
+    *(fe_t*)&red_o[wave][lane * EPT] = acc;
+    if (lane == 0) {
+        red_m[wave] = M;
+        red_l[wave] = L;
+    }
+    __syncthreads();
+    if (wave != 0 || lane >= D / 4)
+        return;
+    float m = -FLT_MAX, l = 0.f;
+#pragma unroll
+    for (int w = 0; w < MRG_WAVES; ++w)
+        m = fmaxf(m, red_m[w]);
+    f32x4_t o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < MRG_WAVES; ++w) {
+        const float f = __builtin_amdgcn_exp2f(red_m[w] - m);
+        l += f * red_l[w];
+        o += *(const f32x4_t*)&red_o[w][4 * lane] * f;
+    }
+    kv4_store_o<DT>(p, b, hk, row, 4 * lane, o * (l > 0.f ? 1.0f / l : 0.f));
+    if (lane == 0)
+        kv4_store_lse(p, b, hk, row, m, l);
+}
+
+constexpr int kv4_width(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+// Fills in what the sizes decide: R, rows, nchunks, P, least, and the workspace.
+bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t* bytes)
+{
+    const long long R = (long long)(Hq / Hkv) * Sq;
+    const int rows = R <= 16 ? 16 : 32;
+    const long long nchunks = (R + rows - 1) / rows;
+    if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535)
+        return false;
+    const long long nblk = (S + KV_BLK - 1LL) / KV_BLK;
+    const long long least = KV_WAVES;
+    const long long each = (nblk + least - 1) / least;              // splits that a full sequence can have
+    long long P = KV_TARGET / (Hkv * nchunks);
+    P = P < B ? B : P < B * each ? P : B * each;
+    p->R = (int)R;
+    p->rows = rows;
+    p->nchunks = (int)nchunks;
+    p->P = (int)P;
+    p->least = (int)least;
+    *bytes = P > B ? ((size_t)Hkv * nchunks * P * rows * (kv4_width(D) + 2) * sizeof(float) + (size_t)B * 2 * sizeof(int) + 15) / 16 * 16 : 16;
+    return true;
+}
+
+template <int D, int DT>
+int launch_kv4(const Kv4Params& p, hipStream_t stream)
+{
+    const dim3 grid((unsigned)p.P, (unsigned)p.nchunks, (unsigned)p.Hkv);
+    if (p.rows == 16)
+        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 1>), grid, dim3(KV_WAVES * 64), 0, stream, p);
+    else
+        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 2>), grid, dim3(KV_WAVES * 64), 0, stream, p);
+    const int rc = launched();
+    if (rc != NAUT_OK || p.P <= p.B)  // one split each
+        return rc;
+    hipLaunchKernelGGL((naut_decode_kv4_merge_kernel<D, DT>), dim3((unsigned)p.R, (unsigned)p.Hkv, (unsigned)p.B), dim3(MRG_WAVES * 64), 0, stream, p);
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+int naut_kv4_scale_bytes(int D) { return D <= 0 || D % MX != 0 || D > 256 ? 0 : D <= 64 ? 2 : D <= 128 ? 4 : 8; }
+
+int naut_kv4_store(const void* k, const void* v, const naut_kv4_cache* cache, const int* slots, int T, int in_dtype,
+                   const naut_strides* st, void* stream)
+{
+    RowParams p;
+    const int rc = rows_of(k, v, cache, slots, T, in_dtype, st, false, &p);
+    if (rc != NAUT_OK || T == 0)
+        return rc;
+    const dim3 grid((unsigned)(((long long)T * p.Hkv * p.oct + 255) / 256), 2);
+    if (in_dtype == NAUT_BF16)
+        hipLaunchKernelGGL((naut_kv4_store_kernel<NAUT_BF16>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    else
+        hipLaunchKernelGGL((naut_kv4_store_kernel<NAUT_F16>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    return launched();
+}
+
+int naut_kv4_load(void* k, void* v, const naut_kv4_cache* cache, const int* slots, int T, int out_dtype,
+                  const naut_strides* st, void* stream)
+{
+    RowParams p;
+    const int rc = rows_of(k, v, cache, slots, T, out_dtype, st, true, &p);
+    if (rc != NAUT_OK || T == 0)
+        return rc;
+    const dim3 grid((unsigned)(((long long)T * p.Hkv * p.oct + 255) / 256), 2);
+    if (out_dtype == NAUT_BF16)
+        hipLaunchKernelGGL((naut_kv4_load_kernel<NAUT_BF16>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    else
+        hipLaunchKernelGGL((naut_kv4_load_kernel<NAUT_F16>), grid, dim3(256), 0, (hipStream_t)stream, p);
+    return launched();
+}
+
+size_t naut_attn_decode_kv4_workspace_bytes(int B, int Hq, int Hkv, int Sq, int S, int D)
+{
+    Kv4Params p;
+    size_t bytes;
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Sq <= 0 || S <= 0 || Hq % Hkv != 0 || naut_kv4_scale_bytes(D) == 0 ||
+        (long long)B * S > 0x7fffffffLL || !kv4_plan(B, Hq, Hkv, Sq, S, D, &p, &bytes))
+        return 0;
+    return bytes;
+}
+
+int naut_attn_decode_kv4(const void* q, void* o, float* lse, const naut_kv4_cache* cache, const int* lens, int Hq, int Sq,
+                         int causal, float scale, void* workspace, size_t workspace_bytes, void* stream, int in_dtype,
+                         int out_dtype, const naut_strides* st)
+{
+    const int rc = check_cache(cache);
+    if (rc != NAUT_OK)
+        return rc;
+    if (!q || !o)
+        return fail(NAUT_ERR_NULL, "q and o must be non-NULL device pointers");
+    const int B = cache->B, Hkv = cache->Hkv, S = cache->S, D = cache->D;
+    if (Hq <= 0 || Sq <= 0)
+        return fail(NAUT_ERR_SHAPE, "Hq and Sq must be positive");
+    if (Hq % Hkv != 0)
+        return fail(NAUT_ERR_SHAPE, "Hq must be a multiple of the cache's Hkv");
+    if (!std::isfinite(scale))
+        return fail(NAUT_ERR_SHAPE, "scale must be finite");
+    if (scale < 0.f)
+        return fail(NAUT_ERR_UNSUPPORTED, "negative scale is not supported");
+    if ((in_dtype != NAUT_BF16 && in_dtype != NAUT_F16) || (out_dtype != in_dtype && out_dtype != NAUT_F32))
+        return fail(NAUT_ERR_UNSUPPORTED, "supported dtypes: q bf16 or f16; o of the same type or f32");
+    Kv4Params p = {};
+    size_t bytes;
+    if (!kv4_plan(B, Hq, Hkv, Sq, S, D, &p, &bytes))
+        return fail(NAUT_ERR_UNSUPPORTED, "shape exceeds the grid limits");
+    if (((uintptr_t)q | (uintptr_t)o | (uintptr_t)workspace) & 15u)
+        return fail(NAUT_ERR_ALIGN, "q, o and workspace must be 16-byte aligned");
+    if (((uintptr_t)lse | (uintptr_t)lens) & 3u)
+        return fail(NAUT_ERR_ALIGN, "lse and lens must be 4-byte aligned");
+    if (!workspace)
+        return fail(NAUT_ERR_NULL, "workspace must be a non-NULL device pointer");
+    if (workspace_bytes < bytes)
+        return fail(NAUT_ERR_SHAPE, "workspace is smaller than naut_attn_decode_kv4_workspace_bytes()");
+    naut_strides cs = {};  // contiguous [B][Hq][Sq][D]
+    cs.q_s = cs.o_s = D;
+    cs.q_h = cs.o_h = (long long)Sq * D;
+    cs.q_b = cs.o_b = (long long)Hq * Sq * D;
+    if (!st)
+        st = &cs;
+    const long long in_strides[3] = {st->q_b, st->q_h, st->q_s};
+    for (long long x : in_strides)
+        if (x < 0 || x % 8 != 0)
+            return fail(NAUT_ERR_ALIGN, "q strides must be non-negative multiples of 8 elements (16 bytes)");
+    if (st->o_b <= 0 || st->o_h <= 0 || st->o_s <= 0 || st->o_b % 4 != 0 || st->o_h % 4 != 0 || st->o_s % 4 != 0)
+        return fail(NAUT_ERR_ALIGN, "o strides must be positive multiples of 4 elements");
+    if (st->q_s < D || st->o_s < D)
+        return fail(NAUT_ERR_SHAPE, "a sequence stride is smaller than D: rows would overlap");
+    const long long max_rs = 1LL << 23;
+    if (st->q_s > max_rs || st->o_s > max_rs)
+        return fail(NAUT_ERR_UNSUPPORTED, "sequence stride too large");
+
+    const int out_b = out_dtype == NAUT_F32 ? 4 : 2;
+    p.q = q;
+    p.o = o;
+    p.lse = lse;
+    p.codes[0] = (const unsigned char*)cache->k_codes;
+    p.codes[1] = (const unsigned char*)cache->v_codes;
+    p.scales[0] = (const unsigned char*)cache->k_scales;
+    p.scales[1] = (const unsigned char*)cache->v_scales;
+    p.c_b = cache->c_b;
+    p.c_h = cache->c_h;
+    p.c_s = cache->c_s;
+    p.s_b = cache->s_b;
+    p.s_h = cache->s_h;
+    p.s_s = cache->s_s;
+    p.lens = lens;
+    p.ws = (float*)workspace;
+    p.B = B;
+    p.Hq = Hq;
+    p.Hkv = Hkv;
+    p.Sq = Sq;
+    p.S = S;
+    p.causal = causal ? 1 : 0;
+    const float c = scale * 1.4426950408889634f;
+    p.c = c > 0.f ? c : 1.0e-30f;  // scale == 0: every score becomes (almost exactly) 0, the softmax uniform
+    p.out_f32 = out_dtype == NAUT_F32;
+    p.q_bs = st->q_b * 2;
+    p.q_hs = st->q_h * 2;
+    p.q_rs = (int)(st->q_s * 2);
+    p.o_bs = st->o_b * out_b;
+    p.o_hs = st->o_h * out_b;
+    p.o_rs = (int)(st->o_s * out_b);
+    p.nb = D / MX;
+    hipStream_t hs = (hipStream_t)stream;
+    const bool bf = in_dtype == NAUT_BF16;
+    switch (kv4_width(D)) {
+    case 64: return bf ? launch_kv4<64, NAUT_BF16>(p, hs) : launch_kv4<64, NAUT_F16>(p, hs);
+    case 128: return bf ? launch_kv4<128, NAUT_BF16>(p, hs) : launch_kv4<128, NAUT_F16>(p, hs);
+    default: return bf ? launch_kv4<256, NAUT_BF16>(p, hs) : launch_kv4<256, NAUT_F16>(p, hs);
+    }
+}
+
+}  // extern "C"

@@ -1,0 +1,217 @@
+"""naut_attn_fwd_packed against plain 64-bit attention of every sequence: lengths, masks, head dimensions, strides; what lies
+outside the sequences; offsets that make no sense; replays of a captured call that follow the lengths."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_14825_amd import binding as nb
+
+import serving_util as su
+
+pytestmark = pytest.mark.gpu
+
+
+def offsets(lens, first=0):
+    return torch.tensor(np.concatenate([[first], first + np.cumsum(lens)]).astype(np.int32), device="cuda")
+
+
+def reference(q, k, v, q_lens, k_lens, scale, causal, first=0):
+    """Over the rows of the sequences alone: o [T,Hq,D], lse [Hq,T], A, G as the checks want them."""
+    q, k, v = (x.double().cpu().numpy() for x in (q, k, v))
+    Hq, g = q.shape[1], q.shape[1] // k.shape[1]
+    out = [np.zeros_like(q), np.zeros(q.shape[:2]), np.zeros_like(q), np.zeros(q.shape[:2])]
+    a = b = first
+    for Sq, Sk in zip(q_lens, k_lens):
+        for h in range(Hq):
+            for x, y in zip(out, su.reference(q[a : a + Sq, h], k[b : b + Sk, h // g], v[b : b + Sk, h // g], scale, causal)):
+                x[a : a + Sq, h] = y
+        a, b = a + Sq, b + Sk
+    return out
+
+
+def run(q_lens, k_lens, Hq, Hkv, D, causal, dtype="bf16", out="bf16", pad=0, first=0, layout="dense", seed=0, magnify=1.0):
+    k_lens = q_lens if k_lens is None else k_lens
+    what = "packed q %s k %s Hq %d Hkv %d D %d causal %d %s->%s pad %d first %d %s" % (
+        q_lens if len(q_lens) < 20 else len(q_lens), k_lens if len(k_lens) < 20 else len(k_lens), Hq, Hkv, D, causal, dtype, out, pad, first, layout)
+    print(what, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    Tq, Tk = first + sum(q_lens) + pad, first + sum(k_lens) + pad
+
+    def rows(T, H, factor=1.0, kind=dtype):
+        if layout == "heads":     # head-major memory
+            x = torch.empty((H, T, D), device="cuda", dtype=su.TORCH[kind]).transpose(0, 1)
+        elif layout == "fused":   # rows of a wider tensor
+            x = torch.empty((T, H, D + 24), device="cuda", dtype=su.TORCH[kind])[..., 8 : 8 + D]
+        else:
+            x = torch.empty((T, H, D), device="cuda", dtype=su.TORCH[kind])
+        return x.copy_(torch.randn((T, H, D), device="cuda", generator=gen) * factor)
+
+    q, k, v = rows(Tq, Hq, magnify), rows(Tk, Hkv), rows(Tk, Hkv)
+    ref = reference(q, k, v, q_lens, k_lens, 1 / math.sqrt(D), causal, first)
+    o, lse = rows(Tq, Hq, 0.0, out).fill_(7.0), torch.full((Hq, Tq), 7.0, device="cuda")
+    for x in (k, v):  # what belongs to no sequence
+        x[:first] = float("nan")
+        x[first + sum(k_lens) :] = float("nan")
+    cu_q = offsets(q_lens, first)
+    nb.naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_q if k_lens is q_lens else offsets(k_lens, first), causal, 1 / math.sqrt(D))
+    torch.cuda.synchronize()
+    inside = slice(first, first + sum(q_lens))
+    on, ln = o.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert (np.delete(on, np.r_[inside], 0) == 7.0).all() and (np.delete(ln, np.r_[inside], 1) == 7.0).all(), what + ": rows of no sequence"
+    su.check(on[inside], ln.T[inside], (ref[0][inside], ref[1][inside], ref[2][inside], ref[3][inside]), dtype, out, max(list(k_lens) + [1]), what)
+    return o, lse
+
+
+EDGES = [1, 0, 31, 32, 33, 127, 128, 129, 2, 255, 257, 64, 0]
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_lengths_at_the_edges_of_tiles(D, causal):
+    run(EDGES, None, 4, 2, D, causal)
+
+
+@pytest.mark.parametrize("D", [8, 40, 72, 80, 88, 96, 104, 136, 192, 200, 248])
+def test_head_dimensions(D):
+    run([70, 1, 161, 33], None, 2, 1, D, True, "bf16" if D % 16 else "f16", "bf16" if D % 16 else "f16", pad=3)
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f16", "f32")])
+@pytest.mark.parametrize("D", [64, 80, 96, 128, 192, 256])
+def test_types(D, dtype, out):
+    run([200, 5, 77], None, 6, 2, D, True, dtype, out, seed=1)
+
+
+@pytest.mark.parametrize("heads", [(1, 1), (3, 3), (8, 1), (12, 4), (14, 2), (16, 8), (7, 7), (40, 8)])
+def test_head_counts(heads):
+    run([130, 31, 64, 300], None, heads[0], heads[1], 64, True, seed=2)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_more_keys_than_queries(D):
+    run([1, 5, 128, 33, 200, 64], [300, 5, 129, 700, 1100, 65], 4, 1, D, True, seed=3)
+    run([1, 5, 128, 33, 200, 64], [300, 9, 1, 700, 31, 0], 4, 1, D, False, seed=3)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_rows_that_see_nothing(D):
+    """Fewer keys than queries under the mask, no keys at all: o = 0, lse = -inf, beside ordinary rows and tiles."""
+    run([200, 40, 300, 129, 5, 260], [60, 0, 299, 1, 5, 3], 4, 2, D, True, seed=4)
+    run([40, 3, 1], [0, 0, 0], 2, 2, D, False, seed=4)
+    run([40, 3, 1], [0, 0, 0], 2, 2, D, True, "f16", "f32", seed=4)
+
+
+@pytest.mark.parametrize("layout", ["heads", "fused"])
+@pytest.mark.parametrize("D", [64, 72, 128, 192])
+def test_strides_and_offsets_that_do_not_start_at_zero(layout, D):
+    run([100, 1, 190], None, 4, 2, D, True, pad=40, first=37, layout=layout, seed=5)
+
+
+@pytest.mark.parametrize("n", [63, 64, 65, 255, 257, 700])
+def test_many_sequences(n):
+    """One sequence to a lane, four lots of 64 kept in registers, more than that."""
+    rng = np.random.default_rng(n)
+    run([int(x) for x in rng.integers(0, 6, n - 1)] + [140], None, 8, 4, 64, True, seed=6)
+    run([int(x) for x in rng.integers(0, 200, n)] if n < 100 else [1] * (n - 2) + [300, 129], None, 2, 1, 128, True, seed=6)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_maxima_that_move(D):
+    run([600, 129], None, 4, 4, D, True, seed=7, magnify=6.0)
+    run([600, 129], None, 4, 4, D, True, "f16", "f16", seed=7, magnify=6.0)
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,lens", [(128, 32, 8, [1500, 40, 700]), (128, 16, 16, [4100]), (64, 8, 8, [2300, 2000, 1]), (256, 4, 1, [1800, 900]),
+                                           (128, 5, 5, [2600, 2100]), (64, 33, 11, [1000, 600])])
+@pytest.mark.parametrize("causal", [True, False])
+def test_long_sequences(D, Hq, Hkv, lens, causal):
+    run(lens, None, Hq, Hkv, D, causal, seed=8)
+
+
+def test_no_rows():
+    z = torch.zeros((0, 4, 64), device="cuda", dtype=torch.bfloat16)
+    x = torch.full((5, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    nb.naut_attn_fwd_packed(z, z, z, z, None, none, none, True, 0.1)                     # no sequence, no row
+    nb.naut_attn_fwd_packed(x, x, x, o := x.clone(), None, none, none, True, 0.1)        # rows, but no sequence
+    nb.naut_attn_fwd_packed(z, x, x, z, None, offsets([0, 0]), offsets([2, 3]), False, 0.1)
+    nb.naut_attn_fwd_packed(x, z, z, p := x.clone(), None, offsets([5]), offsets([0]), False, 0.1)  # no keys anywhere
+    torch.cuda.synchronize()
+    assert (o == 7.0).all() and (p == 0.0).all()
+
+
+def test_offsets_that_make_no_sense_are_empty_sequences():
+    """Falling, negative, or beyond the tensors: nothing of that sequence is read or written, the others stand."""
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    q, k, v = (torch.randn((300, 2, 64), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
+    whole = reference(q[:100], k[:100], v[:100], [100], [100], 0.125, True)
+    for cu_q, cu_k, left in [([0, 100, 90], [0, 100, 200], 100), ([0, 100, 301], [0, 100, 200], 100), ([0, 100, 200], [0, 100, 1 << 30], 100),
+                             ([0, 100, -5], [0, 100, 200], 100), ([0, 100, 200], [0, 100, 50], 100), ([-7, -3], [0, 10], 0),
+                             ([0, 100, 0x7fffffff], [0, 100, 0x7fffffff], 100)]:
+        print(cu_q, cu_k, flush=True)
+        o, lse = torch.full_like(q, 7.0), torch.full((2, 300), 7.0, device="cuda")
+        as_t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+        nb.naut_attn_fwd_packed(q, k, v, o, lse, as_t(cu_q), as_t(cu_k), True, 0.125)
+        torch.cuda.synchronize()
+        assert (o[left:] == 7.0).all() and (lse[:, left:] == 7.0).all()
+        if left:
+            su.check(o[:100].double().cpu().numpy(), lse[:, :100].T.double().cpu().numpy(), [whole[0], whole[1], whole[2], whole[3]], "bf16", "bf16", 100, "first sequence")
+
+
+def test_calls_repeat_bit_for_bit_and_on_another_stream():
+    a, la = run([333, 1, 90], None, 8, 2, 128, True, seed=10)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        b, lb = run([333, 1, 90], None, 8, 2, 128, True, seed=10)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and torch.equal(la, lb)
+
+
+def test_rows_beyond_2_31_bytes():
+    """Offsets that pass 32 bits: the last of two sequences lies past 4 GiB of a tensor of far-apart rows."""
+    T, H, D, stride = 700, 2, 64, 1 << 22  # 8 MiB a row
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    base = torch.empty(T * stride, device="cuda", dtype=torch.bfloat16)
+    wide = lambda at: torch.as_strided(base, (T, H, D), (stride, D, 1), at)
+    q, k, v, o = (wide(at) for at in (0, 1024, 2048, 4096))
+    for x in (q, k, v):
+        x.copy_(torch.randn((T, H, D), device="cuda", generator=gen))
+    o.fill_(7.0)
+    lse = torch.empty((H, T), device="cuda")
+    lens = [90, 610]
+    nb.naut_attn_fwd_packed(q, k, v, o, lse, offsets(lens), offsets(lens), True, 0.125)
+    torch.cuda.synchronize()
+    ref = reference(q.contiguous(), k.contiguous(), v.contiguous(), lens, lens, 0.125, True)
+    su.check(o.double().cpu().numpy(), lse.T.double().cpu().numpy(), ref, "bf16", "bf16", 610, "far rows")
+
+
+def test_a_captured_call_follows_the_lengths():
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    q, k, v = (torch.randn((500, H, 128), device="cuda", generator=gen).to(torch.bfloat16) for H in (8, 2, 2))
+    o, lse = torch.empty_like(q), torch.empty((8, 500), device="cuda")
+    call = lambda: nb.naut_attn_fwd_packed(q, k, v, o, lse, cu4, cu4, True, 0.09)
+    cu4 = offsets([100, 100, 100, 200])
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for lens in ([100, 100, 100, 200], [1, 498, 0, 1], [0, 0, 0, 500], [130, 7, 260, 3], [100, 100, 100, 200]):
+        cu4.copy_(offsets(lens))
+        q.copy_(torch.randn(q.shape, device="cuda", generator=gen))
+        o.fill_(7.0)
+        lse.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = o.clone(), lse.clone()
+        o.fill_(7.0)
+        lse.fill_(7.0)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, o) and torch.equal(got_lse, lse), lens
+        n = sum(lens)
+        ref = reference(q[:n], k[:n], v[:n], lens, lens, 0.09, True)
+        su.check(o[:n].double().cpu().numpy(), lse[:, :n].T.double().cpu().numpy(), ref, "bf16", "bf16", 500, str(lens))
