@@ -519,11 +519,11 @@ def naut_attn_decode_fp8_strided(q, k, v, o, lse, causal: bool, scale: float, de
         raise NautError(rc, last_error_string())
 
 
-def _one_device(tensors):
-    """The device of all of them; an error where they are not on one GPU."""
-    device = tensors[0].device
+def _one_device(*tensors):
+    """The index of the GPU that all of them are on."""
+    device = tensors[0].get_device()
     for t in tensors:
-        if not t.is_cuda or t.device != device:
+        if t.get_device() != device or device < 0:
             raise ValueError("all tensors must be on one GPU")
     return device
 
@@ -531,7 +531,7 @@ def _one_device(tensors):
 def _call(device, f, *args):
     """f(*args) with `device` current (a launch goes to the current device), its status raised."""
     import torch
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device:
         rc = f(*args)
     else:
         with torch.cuda.device(device):
@@ -548,10 +548,9 @@ def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float
     The queries of a sequence are the last positions of its keys.  Rows of no sequence are left as they are, a row that
     sees no key gets o = 0 and lse = -inf.  Enqueues on `stream` and returns; the lengths are read on the GPU."""
     import torch
-    for t in (q, k, v, o):
-        if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] != 1):
-            raise ValueError("q, k, v, o must be 3-d with a contiguous last axis")
-    device = _one_device((q, k, v, o, cu_q, cu_k) if lse is None else (q, k, v, o, cu_q, cu_k, lse))
+    if q.dim() != 3 or k.dim() != 3 or v.dim() != 3 or o.dim() != 3:
+        raise ValueError("q, k, v, o must be 3-d")
+    device = _one_device(q, k, v, o, cu_q, cu_k) if lse is None else _one_device(q, k, v, o, cu_q, cu_k, lse)
     Tq, Hq, D = q.shape
     Tk, Hkv = k.shape[:2]
     if k.shape != (Tk, Hkv, D) or v.shape != (Tk, Hkv, D) or o.shape != (Tq, Hq, D):
@@ -564,10 +563,15 @@ def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float
     for t in (cu_q, cu_k):
         if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous() or t.numel() != n + 1 or n < 0:
             raise ValueError("cu_q and cu_k must be contiguous int32 tensors of n + 1 offsets each")
-    st = NautStrides(0, q.stride(1), q.stride(0), 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0), 0, o.stride(1), o.stride(0))
+    st = None
+    if not (q.is_contiguous() and k.is_contiguous() and v.is_contiguous() and o.is_contiguous()):
+        if q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1 or o.stride(2) != 1:
+            raise ValueError("q, k, v, o must have a contiguous last axis")
+        st = ctypes.byref(NautStrides(0, q.stride(1), q.stride(0), 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0),
+                                      0, o.stride(1), o.stride(0)))
     _call(device, lib().naut_attn_fwd_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
-          None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, Tq, Tk, Hq, Hkv, D, int(bool(causal)),
-          float(scale), _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o), ctypes.byref(st))
+          None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, Tq, Tk, Hq, Hkv, D, 1 if causal else 0,
+          scale, _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o), st)
 
 
 def kv4_scale_bytes(D: int) -> int:
@@ -587,7 +591,7 @@ class KV4Cache:
         for t in self.tensors:
             if t.dtype != torch.uint8 or t.dim() != 4 or t.stride(3) != 1:
                 raise ValueError("codes and scales must be 4-d uint8 tensors with a contiguous last axis")
-        self.device = _one_device(self.tensors)
+        self.device = _one_device(*self.tensors)
         B, Hkv, S, half = k_codes.shape
         self.B, self.Hkv, self.S, self.D = B, Hkv, S, 2 * half
         if v_codes.shape != k_codes.shape or v_scales.shape != k_scales.shape or k_scales.shape != (B, Hkv, S, kv4_scale_bytes(self.D)):
@@ -610,18 +614,18 @@ class KV4Cache:
 
 def _kv4_rows(f, k, v, cache, slots, stream):
     import torch
-    device = _one_device((k, v, slots))
-    if device != cache.device:
-        raise ValueError("all tensors must be on one GPU")
+    device = _one_device(k, v, slots, cache.tensors[0])
     T = slots.numel()
-    for t in (k, v):
-        if t.dim() != 3 or t.shape != (T, cache.Hkv, cache.D) or t.stride(2) != 1 or t.dtype != k.dtype:
-            raise ValueError("k and v must be [T,Hkv,D] of one dtype with a contiguous last axis, T the number of slots")
+    if k.shape != (T, cache.Hkv, cache.D) or v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must be [T,Hkv,D] of one dtype, T the number of slots")
     if slots.dtype != torch.int32 or slots.dim() != 1 or not slots.is_contiguous():
         raise ValueError("slots must be a contiguous int32 device tensor [T]")
-    st = NautStrides(0, 0, 0, 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0), 0, 0, 0)
-    _call(device, f, k.data_ptr(), v.data_ptr(), cache.ref, slots.data_ptr(), T, _torch_dtype_code(k), ctypes.byref(st),
-          _stream_ptr(stream, k))
+    st = None
+    if not (k.is_contiguous() and v.is_contiguous()):
+        if k.stride(2) != 1 or v.stride(2) != 1:
+            raise ValueError("k and v must have a contiguous last axis")
+        st = ctypes.byref(NautStrides(0, 0, 0, 0, k.stride(1), k.stride(0), 0, v.stride(1), v.stride(0), 0, 0, 0))
+    _call(device, f, k.data_ptr(), v.data_ptr(), cache.ref, slots.data_ptr(), T, _torch_dtype_code(k), st, _stream_ptr(stream, k))
 
 
 def naut_kv4_store(k, v, cache, slots, stream=None):
@@ -647,27 +651,30 @@ def naut_attn_decode_kv4(q, o, lse, cache, lens, causal: bool, scale: float, wor
     has (None: S each), workspace contiguous, at least decode_kv4_workspace_bytes(...) bytes.  Enqueues on `stream`; the
     lengths are read on the GPU."""
     import torch
-    tensors = [q, o, workspace] + [t for t in (lse, lens) if t is not None]
-    device = _one_device(tensors)
-    if device != cache.device:
-        raise ValueError("all tensors must be on one GPU")
-    for t in (q, o):
-        if t.dim() != 4 or t.stride(3) != 1:
-            raise ValueError("q and o must be 4-d with a contiguous last axis")
-    if not workspace.is_contiguous():
-        raise ValueError("workspace must be contiguous")
+    device = _one_device(q, o, workspace, cache.tensors[0])
+    if q.dim() != 4 or o.dim() != 4:
+        raise ValueError("q and o must be 4-d")
     B, Hq, Sq, D = q.shape
     if o.shape != q.shape or B != cache.B or D != cache.D:
         raise ValueError("shape mismatch between q, o and the cache")
-    if lse is not None and not (lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (B, Hq, Sq)):
-        raise ValueError("lse must be a contiguous fp32 device tensor [B,Hq,Sq]")
-    if lens is not None and not (lens.is_contiguous() and lens.dtype == torch.int32 and lens.shape == (B,)):
-        raise ValueError("lens must be a contiguous int32 device tensor [B]")
-    st = NautStrides(*q.stride()[:3], 0, 0, 0, 0, 0, 0, *o.stride()[:3])
-    _call(device, lib().naut_attn_decode_kv4, q.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(), cache.ref,
-          None if lens is None else lens.data_ptr(), Hq, Sq, int(bool(causal)), float(scale), workspace.data_ptr(),
-          workspace.numel() * workspace.element_size(), _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o),
-          ctypes.byref(st))
+    if not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    st = lse_ptr = lens_ptr = None
+    if not (q.is_contiguous() and o.is_contiguous()):
+        if q.stride(3) != 1 or o.stride(3) != 1:
+            raise ValueError("q and o must have a contiguous last axis")
+        st = ctypes.byref(NautStrides(*q.stride()[:3], 0, 0, 0, 0, 0, 0, *o.stride()[:3]))
+    if lse is not None:
+        if not (lse.is_contiguous() and lse.dtype == torch.float32 and lse.shape == (B, Hq, Sq) and lse.get_device() == device):
+            raise ValueError("lse must be a contiguous fp32 device tensor [B,Hq,Sq]")
+        lse_ptr = lse.data_ptr()
+    if lens is not None:
+        if not (lens.is_contiguous() and lens.dtype == torch.int32 and lens.shape == (B,) and lens.get_device() == device):
+            raise ValueError("lens must be a contiguous int32 device tensor [B]")
+        lens_ptr = lens.data_ptr()
+    _call(device, lib().naut_attn_decode_kv4, q.data_ptr(), o.data_ptr(), lse_ptr, cache.ref, lens_ptr, Hq, Sq, 1 if causal else 0,
+          scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, q), _torch_dtype_code(q),
+          _torch_dtype_code(o), st)
 
 
 def naut_probe_mfma(out, work_groups: int, trips: int, kind: int, stream=None) -> float:

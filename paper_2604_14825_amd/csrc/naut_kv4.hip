@@ -240,8 +240,7 @@ int launched()
 // eight of them an A operand, and Q is loaded in the order that this gives the contraction.  V's codes come in the same
 // way, are converted, and pass through the wavefront's own LDS as 16-bit rows to be read transposed.
 constexpr int KV_BLK = 32;    // keys per block
-constexpr int KV_WAVES = 4;   // wavefronts of a split kernel
-constexpr int KV_TARGET = 1024;  // work-groups that the plan aims at: four to a CU
+constexpr int KV_TARGET = 256;  // work-groups that the plan aims at: one to a CU, of eight wavefronts
 constexpr int MRG_WAVES = 4;
 
 struct Kv4Params {
@@ -272,60 +271,59 @@ __device__ __forceinline__ int kv4_len(const Kv4Params& p, int b)
     return n < 0 ? 0 : n < p.S ? n : p.S;
 }
 
-// ceil(x / y) for 0 <= x < 2^26, y > 0: by the reciprocal, and put right
-__device__ __forceinline__ int ceil_div(int x, int y, float rcp)
-{
-    int q = (int)((float)x * rcp);
-    int r = x - q * y;
-    q += r > 0;
-    r -= r > 0 ? y : 0;
-    q += r > 0;
-    r -= r > 0 ? y : 0;
-    return q - (r <= -y);
-}
-
 struct Kv4Split {
     int b, split, nsplit, first;  // sequence, its split, its splits, the index of its first split
     int len, begin, end;          // keys, blocks
 };
 
-// Which part of which sequence split x is: every sequence is cut into equal parts of at most L blocks (an empty one is one
-// part), L the least at which the parts are no more than P, found by halving between the mean and twice the longest.  64
-// sequences at a time, one to a lane.
+// Which part of which sequence split x is: every sequence is cut into equal parts of about L blocks (an empty one is one
+// part), for an L at which they are no more than P.  The mean, total / P, is the least that can do and does where the
+// lengths are alike; total / (P - B) always does, as no sequence has more than a part beyond its share.  Between them by halving, to a
+// sixteenth: a longer search costs more than the shorter splits give (with a full one over the 16 ragged sequences of 24.7 MB
+// of keys and values the call took 1.7 us longer).  64 sequences at a time, one to a lane.
 __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, Kv4Split* out)
 {
+    if (x >= p.P)
+        return false;  // the grid is rounded up
     const int nch = (p.B + 63) >> 6;
     auto blocks = [&](int c) { return c * 64 + lane < p.B ? (kv4_len(p, c * 64 + lane) + KV_BLK - 1) / KV_BLK : -1; };
-    const int mine = blocks(0);  // the first chunk's, kept
+    const int mine = blocks(0);  // the first 64's, kept
     auto of = [&](int c) { return c == 0 ? mine : blocks(c); };
-    auto parts = [&](int n, int L, float rcp) { return n < 0 ? 0 : n == 0 ? 1 : ceil_div(n, L, rcp); };
+    // Parts of a sequence of n blocks.  Need not be the exact quotient: its blocks are dealt out evenly over whatever it is.
+    auto parts = [&](int n, float rcp) {
+        const int m = (int)__builtin_fmaf((float)n, rcp, 0.9999f);
+        return n < 0 ? 0 : m < 1 ? 1 : m;
+    };
     auto count = [&](int L) {
         const float rcp = __builtin_amdgcn_rcpf((float)L);
-        int sum = 0;
-        for (int c = 0; c < nch; ++c)
-            sum += parts(of(c), L, rcp);
+        int sum = parts(mine, rcp);
+        for (int c = 1; c < nch; ++c)
+            sum += parts(blocks(c), rcp);
         return wave_sum(sum);
     };
-    int total = 0;  // blocks, rounded up: in units that do not overflow
+    int total = 0;
     for (int c = 0; c < nch; ++c)
         total += of(c) > 0 ? of(c) : 0;
     total = wave_sum(total);
-    int lo = (total + p.P - 1) / p.P;
-    lo = lo > p.least ? lo : p.least;
-    if (count(lo) > p.P) {
-        int hi = (p.S + KV_BLK - 1) / KV_BLK;  // one part each: B <= P
-        while (lo < hi) {
+    int L = (total + p.P - 1) / p.P;
+    L = L > p.least ? L : p.least;
+    if (count(L) > p.P) {
+        const int longest = (p.S + KV_BLK - 1) / KV_BLK + 1;  // a part each
+        int lo = L, hi = p.P > p.B ? total / (p.P - p.B) + 1 : longest;
+        hi = hi < longest && count(hi) <= p.P ? hi : longest;
+        while (hi - lo > (lo >> 4) + 1) {
             const int mid = (lo + hi) >> 1;
             if (count(mid) <= p.P)
                 hi = mid;
             else
-                lo = mid + 1;
+                lo = mid;
         }
+        L = hi;
     }
-    const float rcp = __builtin_amdgcn_rcpf((float)lo);
+    const float rcp = __builtin_amdgcn_rcpf((float)L);
     int before = 0;
     for (int c = 0; c < nch; ++c) {
-        const int n = of(c), m = parts(n, lo, rcp);
+        const int n = of(c), m = parts(n, rcp);
         const int incl = wave_scan(m) + before;
         const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > x);
         if (mask == 0) {
@@ -383,23 +381,21 @@ __device__ __forceinline__ float group_sum(float x)
     return a + b;
 }
 
-// Byte offset of 16-byte chunk c of V's row r (D 16-bit values) in LDS.  A transposed read takes 32 bytes of each of 16 rows, a
-// write 16 bytes of each of eight: pairs of chunks are XOR-ed with the row so that both go to different banks.
-template <int D>
-__device__ __forceinline__ int v4_off(int r, int c)
-{
-    const int key = D == 64 ? (r >> 1) & 3 : r & 7;
-    return r * (D * 2) + ((c ^ (key << 1)) << 4);
-}
+// Bytes between V's rows in LDS.  A transposed read takes 32 bytes of each of 16 rows, a write 16 bytes of each of eight: with
+// 32 bytes of padding both go to different banks, and every address is one register plus a constant.
+constexpr int v4_row(int D) { return D * 2 + 32; }
+
+// Wavefronts of a split kernel.
+constexpr int kv4_waves(int D, int RT) { return D == 256 && RT == 2 ? 4 : 8; }
 
 template <int D, int DT, int RT>
-__global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv4Params p)
+__global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(const Kv4Params p)
 {
     using X = Mx<DT>;
-    constexpr int NW = KV_WAVES;
+    constexpr int NW = kv4_waves(D, RT);
     constexpr int KS = D / 32;             // words of codes, and MFMAs, per key tile
     constexpr int DT16 = D / 16;           // 16-row tiles of O^T
-    constexpr int VB = KV_BLK * D * 2;     // a block of V in LDS
+    constexpr int VROW = v4_row(D), VB = KV_BLK * VROW;  // a block of V in LDS
     constexpr int OB = RT * 16 * D * 4;    // a wavefront's O
     constexpr int REGION = VB > OB ? VB : OB;
     __shared__ __attribute__((aligned(1024))) unsigned char smem[NW * REGION];
@@ -440,46 +436,48 @@ __global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv
             qf[rt][ks] = dim(ks) < p.nb * MX ? *(const i32x4_t*)(qr + dim(ks) * 2) : i32x4_t{0, 0, 0, 0};
     }
 
+    // Codes and scale bytes of the lane's keys of a block, of K or of V.  The next block's are requested into the same registers
+    // as soon as this block's have been converted.
     struct Block {
-        int w[2][2][KS];   // [K, V][key tile][word]
-        int s[2][2][CH];   // scale bytes
+        int w[2][KS];   // [key tile][word]
+        int s[2][CH];
     };
-    auto load = [&](Block& x, int blk) {
+    const int c_s = (int)p.c_s, s_s = (int)p.s_s;
+    auto load = [&](Block& x, int kv, int blk) {
+        const int left = len - 1 - blk * KV_BLK;  // the ragged last block reads its last key again
+        const unsigned char* const cb = cg[kv] + (long long)blk * (KV_BLK * (long long)c_s);
+        const unsigned char* const sb = sg[kv] + (long long)blk * (KV_BLK * (long long)s_s);
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv)
+        for (int t = 0; t < 2; ++t) {
+            int key = t * 16 + l16;
+            key = key < left ? key : left;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                int key = blk * KV_BLK + t * 16 + l16;
-                key = key < len ? key : len - 1;  // the ragged last block reads its last key again
-                const unsigned char* const cr = cg[kv] + key * p.c_s;
-                const unsigned char* const sr = sg[kv] + key * p.s_s;
+            for (int j = 0; j < CH; ++j) {
+                const unsigned co = (unsigned)(key * c_s + (D == 64 ? (g4 * 8 < p.nb * 16 ? g4 * 8 : 0) : blk_of(j) * 16));
                 if constexpr (D == 64) {
-                    const int at = g4 * 8 < p.nb * 16 ? g4 * 8 : 0;
-                    const i32x2_t y = *(const i32x2_t*)(cr + at);
-                    x.w[kv][t][0] = y.x;
-                    x.w[kv][t][1] = y.y;
+                    const i32x2_t y = *(const i32x2_t*)(cb + co);
+                    x.w[t][0] = y.x;
+                    x.w[t][1] = y.y;
                 } else {
+                    const i32x4_t y = *(const i32x4_t*)(cb + co);
 #pragma unroll
-                    for (int j = 0; j < CH; ++j) {
-                        const i32x4_t y = *(const i32x4_t*)(cr + blk_of(j) * 16);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            x.w[kv][t][4 * j + i] = y[i];
-                    }
+                    for (int i = 0; i < 4; ++i)
+                        x.w[t][4 * j + i] = y[i];
                 }
-#pragma unroll
-                for (int j = 0; j < CH; ++j)
-                    x.s[kv][t][j] = sr[blk_of(j)];
+                x.s[t][j] = sb[(unsigned)(key * s_s + blk_of(j))];
             }
+        }
     };
     // eight values of word ks
-    auto values = [&](const Block& x, int kv, int t, int ks) -> i32x4_t {
-        const float s = mx_scale(X::scale_of(x.s[kv][t][CH == 1 ? 0 : ks >> 2]));
-        const int w = x.w[kv][t][ks];
+    auto values = [&](const Block& x, int t, int ks) -> i32x4_t {
+        const float s = mx_scale(X::scale_of(x.s[t][CH == 1 ? 0 : ks >> 2]));
+        const int w = x.w[t][ks];
         return i32x4_t{X::template decode<0>(w, s), X::template decode<1>(w, s), X::template decode<2>(w, s), X::template decode<3>(w, s)};
     };
 
-    unsigned char* const my = smem + wave * REGION;
+    // where the lane writes its values of V's key l16, and reads keys 4 g4 .. 4 g4 + 3 of 16 columns transposed
+    unsigned char* const v_write = smem + wave * REGION + l16 * VROW + dim(0) * 2;
+    const unsigned char* const v_read = smem + wave * REGION + (4 * g4 + (l16 >> 2)) * VROW + (l16 & 3) * 8;
     f32x4_t oacc[RT][DT16];
     float m_run[RT], l_run[RT];  // reference maximum (log2 units, the lowest value there is at first), the lane's share of the sum
 #pragma unroll
@@ -491,9 +489,14 @@ __global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv
         l_run[rt] = 0.f;
     }
 
-    for (int blk = sp.begin + wave; blk < sp.end; blk += NW) {
-        Block x;
-        load(x, blk);
+    Block kx, vx;
+    int blk = sp.begin + wave;
+    if (blk < sp.end) {
+        load(kx, 0, blk);
+        load(vx, 1, blk);
+    }
+    for (; blk < sp.end; blk += NW) {
+        const int nxt = blk + NW < sp.end ? blk + NW : blk;  // the last one's loads are for nobody, and cost less than a branch
         f32x4_t s[RT][2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -502,21 +505,23 @@ __global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv
                 s[rt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {
-                const i32x4_t kf = values(x, 0, t, ks);
+                const i32x4_t kf = values(kx, t, ks);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
                     s[rt][t] = X::mfma(kf, qf[rt][ks], s[rt][t]);
             }
         }
+        load(kx, 0, nxt);
         // V to LDS, as rows of 16-bit values
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                *(i32x4_t*)(my + v4_off<D>(t * 16 + l16, dim(ks) >> 3)) = values(x, 1, t, ks);
+                *(i32x4_t*)(v_write + t * 16 * VROW + (ks >> 2) * 256 + (ks & 3) * 16) = values(vx, t, ks);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        load(vx, 1, nxt);
         const int key0 = blk * KV_BLK;
         i32x4_t pb[RT];
 #pragma unroll
@@ -553,10 +558,8 @@ __global__ __launch_bounds__(KV_WAVES * 64) void naut_decode_kv4_kernel(const Kv
         // A lane's eight keys of P are 4 g4 + {0..3} of either key tile: so are those of the V^T fragments.
 #pragma unroll
         for (int dt = 0; dt < DT16; ++dt) {
-            const int r = 4 * g4 + (l16 >> 2), d = 16 * dt + 4 * (l16 & 3);
-            const unsigned char* const a = my + v4_off<D>(r, d >> 3) + (d & 7) * 2;
-            const i16x4_t r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(a));
-            const i16x4_t r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(a + 16 * D * 2));
+            const i16x4_t r0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(v_read + dt * 32));
+            const i16x4_t r1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((NAUT_LDS i16x4_t*)(v_read + dt * 32 + 16 * VROW));
             const i32x2_t lo = __builtin_bit_cast(i32x2_t, r0), hi = __builtin_bit_cast(i32x2_t, r1);
             const i32x4_t vf = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
@@ -706,9 +709,9 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
     if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535)
         return false;
     const long long nblk = (S + KV_BLK - 1LL) / KV_BLK;
-    const long long least = KV_WAVES;
-    const long long each = (nblk + least - 1) / least;              // splits that a full sequence can have
+    const long long least = kv4_waves(kv4_width(D), rows / 16);  // a block for every wavefront
     long long P = KV_TARGET / (Hkv * nchunks);
+    const long long each = nblk <= 2 * least ? 1 : (nblk + least - 1) / least;  // splits that a full sequence can have
     P = P < B ? B : P < B * each ? P : B * each;
     p->R = (int)R;
     p->rows = rows;
@@ -722,11 +725,13 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
 template <int D, int DT>
 int launch_kv4(const Kv4Params& p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)p.P, (unsigned)p.nchunks, (unsigned)p.Hkv);
+    // Work-groups are dealt to the XCDs by linear id mod 8: rounded up to eights, the same split of every K/V head and chunk is on
+    // one XCD, whose L2 serves the chunks from one read and the heads of a sequence-major cache from whole lines.
+    const dim3 grid((unsigned)(p.P + 7) / 8 * 8, (unsigned)p.nchunks, (unsigned)p.Hkv);
     if (p.rows == 16)
-        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 1>), grid, dim3(KV_WAVES * 64), 0, stream, p);
+        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 1>), grid, dim3(kv4_waves(D, 1) * 64), 0, stream, p);
     else
-        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 2>), grid, dim3(KV_WAVES * 64), 0, stream, p);
+        hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 2>), grid, dim3(kv4_waves(D, 2) * 64), 0, stream, p);
     const int rc = launched();
     if (rc != NAUT_OK || p.P <= p.B)  // one split each
         return rc;
