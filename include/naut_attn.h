@@ -256,8 +256,8 @@ size_t naut_attn_decode_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * and lse that belong to no sequence are left as they are, and rows of k and v outside a sequence do not reach its results,
  * whatever they hold.  A pair of offsets that falls, is negative or passes Tq or Tk makes its sequence empty.
  * `st` gives the head and sequence (row) strides in elements, by the rules of naut_attn_fwd_strided; the batch strides are not
- * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Tq and Tk at most 2^30, n at most
- * 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
+ * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Hq/Hkv at most 1024, Tq and Tk times that
+ * at most 2^30, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
  */
 int naut_attn_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_q,
                          const int* cu_k, int n, int Tq, int Tk, int Hq, int Hkv, int D, int causal, float scale,

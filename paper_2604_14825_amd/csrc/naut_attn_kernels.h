@@ -222,18 +222,25 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 
     // Tile scheduler: heaviest (last) query tiles first; consecutive block ids walk the
     // (batch, head) axis so that each XCD (block id mod 8) keeps to a fixed subset of heads.
-    int qt, hq, Sq, Sk;
+    int qt, hq, Sq, Sk;  // (PACKED: hq is the first of the K/V head's, Sq counts rows)
     long long q_first, k_first, v_first, o_first, lse_first;  // bytes (lse: values) to the sequence's first row
+    int ahead = 0;                   // keys before the first query's own
+    int pos0 = 0, head0 = 0;         // PACKED: position and head of the tile's first row
+    int pos_end = 0;                 // and the position behind its last row's
     if constexpr (PACKED) {
-        const PackedTile t = packed_tile<BM>(p, blockIdx.x, lane);
+        const PackedTile t = packed_tile<BM>(p, lane);
         if (t.qt < 0)
             return;
         qt = t.qt;
-        hq = t.hq;
-        Sq = t.Sq;
+        hq = t.hk * p.g;
+        Sq = t.rows;
         Sk = t.Sk;
-        if (Sk == 0 || (CAUSAL && (qt + 1) * BM + Sk <= Sq)) {
-            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, hq, t.q0 + qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
+        ahead = Sk - t.Sq;
+        pos0 = p.pos_per_tile ? qt * p.pos_per_tile : qt * BM / p.g;
+        head0 = qt * BM - pos0 * p.g;
+        pos_end = packed_row(p, pos0, head0, (Sq - qt * BM < BM ? Sq - qt * BM : BM) - 1).pos + 1;
+        if (Sk == 0 || (CAUSAL && pos_end + ahead <= 0)) {
+            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, t, qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
             return;
         }
         q_first = (long long)t.q0 * p.q_rs;
@@ -268,7 +275,6 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
         o_first = b * p.o_bs;
         lse_first = (long long)bh * p.S;
     }
-    const int ahead = PACKED ? Sk - Sq : 0;  // keys before the first query's own
     const int hk = hq / (p.Hq / p.Hkv);
 
     const unsigned char* qg = (const unsigned char*)p.q + q_first + hq * p.q_hs;
@@ -282,12 +288,21 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 
     // Q^T fragments (MFMA B operand): lane holds q[my_q][16*ks + 8*h .. +8].
     i32x4_t qf[KS];
+    const unsigned char* q_row = qg + (size_t)my_q_ld * p.q_rs;
+    int sees = my_q, wave_sees = q_wave0, wave_sees_last = q_wave0 + 31;  // the last key that the lane's row, and the wavefront's first and last, may see
+    if constexpr (PACKED) {
+        const PackedRow r = packed_row(p, pos0, head0, my_q_ld - qt * BM);
+        q_row = qg + (long long)r.pos * p.q_rs + r.head * p.q_hs;
+        sees = r.pos + ahead;
+        wave_sees = packed_row(p, pos0, head0, wave * 32).pos + ahead;
+        wave_sees_last = packed_row(p, pos0, head0, wave * 32 + 31).pos + ahead;
+    }
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         // Unconditional, from a chunk that exists (a load under a condition becomes a branch); the padding
         // chunks of a narrower head are zeroed when Q is pinned.
         const int ch = ks * 2 + h < cpr ? ks * 2 + h : cpr - 1;
-        qf[ks] = *(const i32x4_t*)(qg + (size_t)my_q_ld * p.q_rs + ch * 16);
+        qf[ks] = *(const i32x4_t*)(q_row + ch * 16);
     }
     // Keep Q resident: without this the compiler re-issues the global loads inside the key loop.
     // The wide instantiation keeps it, and O, in the accumulation registers.  D <= 128 pins it only
@@ -310,7 +325,8 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
     if constexpr (WIDE)
         pin_q(cpr);
 
-    const int kv_end = CAUSAL ? (Sk < (qt + 1) * BM + ahead ? Sk : (qt + 1) * BM + ahead) : Sk;
+    const int kv_last = PACKED ? pos_end + ahead : (qt + 1) * BM;
+    const int kv_end = CAUSAL && kv_last < Sk ? kv_last : Sk;
     const int ntiles = (kv_end + BN - 1) / BN;
 
     // Lane i of direct load n fills physical chunk P = (wave*LDW + n)*64 + i of the tile, so it fetches the
@@ -497,7 +513,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
 
         // Causal block skipping per wavefront: nothing to do if every key of the tile lies
         // beyond this wavefront's last query.
-        const bool active = (!CAUSAL || kv0 <= q_wave0 + 31 + ahead) && (NG == 1 || j < my_tiles);
+        const bool active = (!CAUSAL || kv0 <= wave_sees_last) && (NG == 1 || j < my_tiles);
         if (active) {
             f32x16_t sacc[KB];
 #pragma unroll
@@ -536,14 +552,14 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
                 }
             }
             // Mask only where the tile straddles the diagonal or the end of the sequence.
-            const bool need_mask = (CAUSAL && kv0 + BN - 1 > q_wave0 + ahead) || (kv0 + BN > Sk);
+            const bool need_mask = (CAUSAL && kv0 + BN - 1 > wave_sees) || (kv0 + BN > Sk);
             if (need_mask) {
 #pragma unroll
                 for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int key = kv0 + kb * 32 + 8 * (r >> 2) + 4 * h + (r & 3);
-                        const bool dead = (CAUSAL && key > my_q + ahead) || key >= Sk;
+                        const bool dead = (CAUSAL && key > sees) || key >= Sk;
                         sacc[kb][r] = dead ? -INFINITY : sacc[kb][r];
                     }
             }
@@ -691,9 +707,22 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
     float inv_l = 1.0f / (l_tot + (dl_run + __shfl_xor(dl_run, 32)));
     if constexpr (PACKED)
         inv_l = l_tot > 0.f ? inv_l : 0.f;  // a row that sees nothing: O = 0, and lse is -inf by itself
+    long long lse_at = lse_first + my_q;
+    if constexpr (PACKED) {
+        const PackedRow r = packed_row(p, pos0, head0, my_q - qt * BM);
+        lse_at = lse_first + (long long)r.head * p.Tq + r.pos;
+    }
     if (my_q < Sq && p.lse != nullptr && h == 0)
-        p.lse[lse_first + my_q] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
+        p.lse[lse_at] = (m_run + __builtin_amdgcn_logf(l_tot)) * 0.6931471805599453f;
     unsigned char* const o_bh = (unsigned char*)p.o + o_first + hq * p.o_hs;
+    auto o_row = [&](int q) {
+        if constexpr (PACKED) {
+            const PackedRow r = packed_row(p, pos0, head0, q - qt * BM);
+            return o_bh + (long long)r.pos * p.o_rs + r.head * p.o_hs;
+        } else {
+            return o_bh + (size_t)q * p.o_rs;
+        }
+    };
     if constexpr (DT_OUT != NAUT_F32) {
         // 16-bit O leaves through LDS in whole rows: a lane owns 4 consecutive d of one query (8 bytes, 32
         // different rows per store instruction); after the exchange D/8 lanes write one row with 16 bytes
@@ -735,11 +764,11 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
             for (int i = 0; i < BATCH; ++i) {
                 const int q = q_wave0 + (i0 + i) * RPI + ln / CPRO;
                 if (q < Sq && ln % CPRO < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
-                    *(i32x4_a8*)(o_bh + (size_t)q * p.o_rs + (ln % CPRO) * 16) = rows[i];
+                    *(i32x4_a8*)(o_row(q) + (ln % CPRO) * 16) = rows[i];
             }
         }
     } else if (my_q < Sq) {
-        unsigned char* og = o_bh + (size_t)my_q * p.o_rs;
+        unsigned char* og = o_row(my_q);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll

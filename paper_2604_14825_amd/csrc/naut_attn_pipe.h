@@ -73,7 +73,8 @@ struct Pieces {
 template <int D, int QH, int NWV, int NG>
 constexpr int pipe_waves_per_simd() { return D <= 64 && QH == 1 && NG == 1 ? 3 : 2; }
 
-// PACKED: sequences back to back (naut_packed.h), Sq queries at the end of Sk keys; rows may see nothing.
+// PACKED: sequences back to back (naut_packed.h), Sq queries at the end of Sk keys; the "queries" of a tile are rows of all the
+// heads that share a K/V head, and may see nothing.
 template <int D, int DT_IN, int DT_OUT, bool CAUSAL, int QH, int NWV, int NG = 1, bool PACKED = false>
 __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>())) void naut_fwd_kernel_pipe(const ParamsOf<PACKED> p)
 {
@@ -119,18 +120,25 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     // causal, D = 64, twelve heads to an XCD: six and six 76.2 us, all at once 65.7; 128 heads, S = 4096, D = 128 eight at a time 529,
     // sixteen 540; 256 heads, S = 640, causal, D = 64 groups 30.8, all 27.2; without the mask a group's tiles are alike, and
     // groups cost nothing).
-    int qt, hq, Sq, Sk;
+    int qt, hq, Sq, Sk;  // (PACKED: hq is the first of the K/V head's, Sq counts rows)
     long long q_first, k_first, v_first, o_first, lse_first;  // bytes (lse: values) to the sequence's first row
+    int ahead = 0;                   // keys before the first query's own
+    int pos0 = 0, head0 = 0;         // PACKED: position and head of the tile's first row
+    int pos_end = 0;                 // and the position behind its last row's
     if constexpr (PACKED) {
-        const PackedTile t = packed_tile<BM>(p, blockIdx.x, lane);
+        const PackedTile t = packed_tile<BM>(p, lane);
         if (t.qt < 0)
             return;
         qt = t.qt;
-        hq = t.hq;
-        Sq = t.Sq;
+        hq = t.hk * p.g;
+        Sq = t.rows;
         Sk = t.Sk;
-        if (Sk == 0 || (CAUSAL && (qt + 1) * BM + Sk <= Sq)) {
-            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, hq, t.q0 + qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
+        ahead = Sk - t.Sq;
+        pos0 = p.pos_per_tile ? qt * p.pos_per_tile : qt * BM / p.g;
+        head0 = qt * BM - pos0 * p.g;
+        pos_end = packed_row(p, pos0, head0, (Sq - qt * BM < BM ? Sq - qt * BM : BM) - 1).pos + 1;
+        if (Sk == 0 || (CAUSAL && pos_end + ahead <= 0)) {
+            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, t, qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
             return;
         }
         q_first = (long long)t.q0 * p.q_rs;
@@ -168,7 +176,6 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         o_first = b * p.o_bs;
         lse_first = (long long)bh * p.S;
     }
-    const int ahead = PACKED ? Sk - Sq : 0;  // keys before the first query's own
     const int hk = hq / (p.Hq / p.Hkv);
     const float c = p.c;
     const float p_limit = p.p_limit;
@@ -188,22 +195,34 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
 
     // Q^T fragments (MFMA B operands), resident for the whole kernel.
     i32x4_t qf[QH][KS];
+    int q_see[QH];  // PACKED: the last key that the lane's row sees
 #pragma unroll
     for (int hf = 0; hf < QH; ++hf) {
         const int q_ld = qrow[hf] < Sq ? qrow[hf] : Sq - 1;
+        const unsigned char* q_row = qg + (size_t)q_ld * p.q_rs;
+        if constexpr (PACKED) {
+            const PackedRow r = packed_row(p, pos0, head0, q_ld - qt * BM);
+            q_row = qg + (long long)r.pos * p.q_rs + r.head * p.q_hs;
+            q_see[hf] = r.pos + ahead;
+        }
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
             // Unconditional, from a chunk that exists; the padding chunks of a narrower head are zeroed when Q is pinned
             // below.  (A load under a condition becomes a branch, and the compiler then waited for the first loads in
             // the middle of issuing the rest.)
             const int ch = ks * 2 + h < cpr ? ks * 2 + h : cpr - 1;
-            qf[hf][ks] = *(const i32x4_t*)(qg + (size_t)q_ld * p.q_rs + ch * 16);
+            qf[hf][ks] = *(const i32x4_t*)(q_row + ch * 16);
         }
     }
-    const int kv_end_wg = CAUSAL ? (Sk < (qt + 1) * BM + ahead ? Sk : (qt + 1) * BM + ahead) : Sk;
-    int kv_end_w = Q0 >= Sq ? 0 : (CAUSAL ? (Sk < Q0 + WQ + ahead ? Sk : Q0 + WQ + ahead) : Sk);
-    if constexpr (PACKED)
-        kv_end_w = kv_end_w > 0 ? kv_end_w : 0;
+    int kv_end_wg = Sk, kv_end_w = Q0 >= Sq ? 0 : Sk;
+    if constexpr (CAUSAL && PACKED) {
+        const int w = packed_row(p, pos0, head0, (Sq - Q0 < WQ ? Sq - Q0 : WQ) - 1 + wave * WQ).pos + 1 + ahead;
+        kv_end_wg = Sk < pos_end + ahead ? Sk : pos_end + ahead;
+        kv_end_w = Q0 >= Sq || w < 0 ? 0 : w < Sk ? w : Sk;
+    } else if constexpr (CAUSAL) {
+        kv_end_wg = Sk < (qt + 1) * BM ? Sk : (qt + 1) * BM;
+        kv_end_w = Q0 >= Sq ? 0 : Sk < Q0 + WQ ? Sk : Q0 + WQ;
+    }
     const int ntiles = (kv_end_wg + BN - 1) / BN;
     // tiles and blocks below count those of a key group: grp, grp + NG, ...
     auto of_group = [&](int n) { return n > grp ? (n - grp + NG - 1) / NG : 0; };
@@ -314,12 +333,16 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             const int key = key0 + 8 * (r >> 2) + (r & 3);
 #pragma unroll
             for (int hf = 0; hf < QH; ++hf)
-                s_[hf][r] = (key >= kv_end_w || (CAUSAL && key > qrow[hf] + ahead)) ? -INFINITY : s_[hf][r];
+                s_[hf][r] = (key >= kv_end_w || (CAUSAL && key > (PACKED ? q_see[hf] : qrow[hf]))) ? -INFINITY : s_[hf][r];
         }
     };
-    // first block that needs masking: 32k+31 > Q0 + ahead (causal; Q0 is a multiple of 32) or 32k+32 > kv_end_w
+    // first block that needs masking: 32k+31 beyond what the first row sees (Q0, causal; a multiple of 32) or 32k+32 > kv_end_w
     const int kc2 = kv_end_w / BN;
-    const int kc1 = !PACKED ? Q0 / BN : Q0 + ahead < 0 ? 0 : (Q0 + ahead + 1) / BN;
+    int kc1 = Q0 / BN;
+    if constexpr (PACKED) {
+        const int sees = packed_row(p, pos0, head0, wave * WQ).pos + ahead;  // (a wavefront beyond the rows has no blocks)
+        kc1 = sees < 0 ? 0 : (sees + 1) / BN;
+    }
     const int k_mask_from = of_group(CAUSAL ? (kc1 < kc2 ? kc1 : kc2) : kc2);
     // max of three; the device code is compiled with NaNs assumed absent, so this is one v_max3_f32 with no quieting of
     // the operands
@@ -715,6 +738,14 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         return;
     constexpr int OUTB = DT_OUT == NAUT_F32 ? 4 : 2;
     unsigned char* const o_bh = (unsigned char*)p.o + o_first + hq * p.o_hs;
+    auto o_row = [&](int q) {
+        if constexpr (PACKED) {
+            const PackedRow r = packed_row(p, pos0, head0, q - qt * BM);
+            return o_bh + (long long)r.pos * p.o_rs + r.head * p.o_hs;
+        } else {
+            return o_bh + (size_t)q * p.o_rs;
+        }
+    };
     // 16-bit O leaves through LDS in whole rows: a lane owns 4 consecutive d of one query (8 bytes, 32 different rows per
     // store instruction); after the exchange 16 lanes (D = 128) write one 256-byte row with 16 bytes each.
     constexpr int CPRO = W / 8, R256 = ROWB >= 256 ? 1 : 256 / ROWB;  // 16-byte chunks per row, rows per 256-byte bank line
@@ -730,9 +761,14 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         float inv_l = 1.0f / (lt + half_sum(dl_run[hf]));  // rows beyond Sq: never stored
         if constexpr (PACKED)
             inv_l = lt > 0.f ? inv_l : 0.f;  // a row that sees nothing: O = 0, and lse is -inf by itself
+        long long lse_at = lse_first + q;
+        if constexpr (PACKED) {
+            const PackedRow r = packed_row(p, pos0, head0, q - qt * BM);
+            lse_at = lse_first + (long long)r.head * p.Tq + r.pos;
+        }
         if (p.lse != nullptr && h == 0 && q < Sq)
-            p.lse[lse_first + q] = (m_run[hf] + __builtin_amdgcn_logf(lt)) * 0.6931471805599453f;
-        unsigned char* const og = o_bh + (size_t)(q < Sq ? q : 0) * p.o_rs;
+            p.lse[lse_at] = (m_run[hf] + __builtin_amdgcn_logf(lt)) * 0.6931471805599453f;
+        unsigned char* const og = o_row(q < Sq ? q : PACKED ? qt * BM : 0);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -762,7 +798,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             const int ch = lane % CPRO;
             const int q = Q0 + i * RPI + lane / CPRO;
             if (q < Sq && ch < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
-                *(i32x4_a8*)(o_bh + (size_t)q * p.o_rs + ch * 16) = rows[i];
+                *(i32x4_a8*)(o_row(q) + ch * 16) = rows[i];
         }
     }
 }

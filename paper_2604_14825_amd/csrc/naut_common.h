@@ -219,6 +219,29 @@ __device__ __forceinline__ int wave_scan(int x)
     x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // row_bcast:31
     return x;
 }
+// N of them at once: the wait states of one are the steps of another
+template <int N>
+__device__ __forceinline__ void wave_scan(int (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x111, 0xf, 0xf, false);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x112, 0xf, 0xf, false);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x114, 0xf, 0xf, false);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x118, 0xf, 0xf, false);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x142, 0xa, 0xf, false);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        x[i] += __builtin_amdgcn_update_dpp(0, x[i], 0x143, 0xc, 0xf, false);
+}
 __device__ __forceinline__ int wave_sum(int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); }
 
 // ---- FP8 (E4M3) pieces shared by the prefill and the decode kernel ----------------------------

@@ -13,16 +13,36 @@ struct PackedParams : Params {  // batch strides, S and the counts of tiles are 
     const int* cu_k;
     int n;        // sequences
     int Tq, Tk;   // rows of q and o, and of k and v: no offset reaches beyond them
+    int g;        // query heads per K/V head, at most 1024
+    unsigned g_inv;  // ceil(2^22 / g)
+    int pos_per_tile;  // positions of a tile where they are whole, otherwise 0
+    int class_of[6];   // levels at which a class of tiles ends (see packed_tile), falling
 };
 
 template <bool PACKED>
 using ParamsOf = std::conditional_t<PACKED, PackedParams, Params>;
 
+// The rows of a tile are (position, query head) pairs of one K/V head, the heads of a position next to each other: row r of a
+// sequence is position r / g of head hk g + r % g.  Sequences that fill no tile of their own waste g times fewer rows than
+// with a tile per head, and the rows of a tile end at nearly the same key (64/8 heads, 8 sequences of 1 to 700 new positions
+// behind 333 to 8100 keys, D = 128: MEASURED_TURNS).
 struct PackedTile {
-    int qt, hq;      // query tile of its sequence (-1: no tile is left for this work-group), query head
+    int qt, hk;      // tile of its sequence's rows (-1: no tile is left for this work-group), K/V head
     int q0, k0;      // the sequence's first row of q and of k
     int Sq, Sk;
+    int rows;        // Sq * g
 };
+
+// Position and head (of the g) of the row x of a tile whose first row is position `pos` of head `head`; x + head < 1280 (BM + g),
+// for which the product is exact: (x + head) g < 2^22.
+struct PackedRow {
+    int pos, head;
+};
+__device__ __forceinline__ PackedRow packed_row(const PackedParams& p, int pos, int head, int x)
+{
+    const unsigned y = (unsigned)(x + head), d = y * p.g_inv >> 22;
+    return {pos + (int)d, (int)(y - d * (unsigned)p.g)};
+}
 
 // Offsets that do not rise, or that leave the tensors, make an empty sequence: no address comes from them.
 struct PackedSeq {
@@ -35,123 +55,137 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b)
     return {q0, k0, ok ? q1 - q0 : 0, ok ? k1 - k0 : 0};
 }
 
-// Tile `bid` of a launch over the n sequences, in tiles of BM queries.  The order is that of one long causal sequence,
-// heaviest first: the last tile of a sequence has the level ceil(Sk / BM) (at least its number of tiles), those before it
-// one less each, and all tiles of a level come before the next.  F(L), the tiles at level L or above, is a sum over the
-// sequences; tile i is at the largest L with F(L) > i, found by halving.  Work-groups are dealt to the XCDs by block id
-// mod 8: where eight divides the query heads, an XCD keeps to an eighth of them, which share their K/V heads' rows in its L2.
+// The work-group's tile, of BM rows.  Heavy tiles come first, as in one long causal sequence: the last tile of a sequence has the
+// level ceil(Sk g / BM) (at least its number of tiles), those before it one less each, and the tiles go by classes of levels,
+// each half as high as the one before (8, 4, 2, 1, 1/2 and 1/4 of the mean level, which the host knows, and the rest).  Inside
+// a class they go by sequence and fall.  F(L), the tiles at level L or above, is a sum over the sequences, one to a
+// lane; those of all classes are formed at once, so that the steps of one sum hide the latency of another's.  The exact order
+// by levels, found by halving, took every work-group about 1 us longer (64 sequences of 256, 32/8 heads, D = 128, no mask:
+// MEASURED_SEARCH).  Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
+// first axis, an XCD keeps to an eighth of them, whose rows stay in its L2.
 template <int BM>
-__device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int bid, int lane)
+__device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lane)
 {
     PackedTile t;
-    int i;
-    if (p.Hq & 7) {
-        i = bid / p.Hq;
-        t.hq = bid % p.Hq;
-    } else {
-        const int hpx = p.Hq >> 3, s = bid >> 3;
-        i = s / hpx;
-        t.hq = (bid & 7) * hpx + s % hpx;
-    }
+    const int x = blockIdx.x, i = (int)(blockIdx.y + blockIdx.z * gridDim.y);
+    t.hk = p.Hkv & 7 ? x : (x & 7) * (p.Hkv >> 3) + (x >> 3);
+    t.qt = -1;
     const int nch = (p.n + 63) >> 6;  // 64 sequences at a time
-    constexpr int KEPT = 4;           // chunks that stay in registers; later ones are read again for every sum
+    constexpr int KEPT = 8;           // lots of them that stay in registers; later ones are read again
+    constexpr int NC = 7;             // classes
+    PackedSeq first = {0, 0, 0, 0};   // of the first 64, for their sequences' own numbers
     int nqt[KEPT], top[KEPT];
     auto load = [&](int c, int& tiles, int& level) {
         tiles = level = 0;
         if (c * 64 + lane < p.n) {
             const PackedSeq s = packed_seq(p, c * 64 + lane);
-            tiles = (s.Sq + BM - 1) / BM;
-            const int keys = (s.Sk + BM - 1) / BM;
+            tiles = (s.Sq * p.g + BM - 1) / BM;
+            const int keys = (s.Sk * p.g + BM - 1) / BM;
             level = tiles > keys ? tiles : keys;
+            if (c == 0)
+                first = s;
         }
     };
-    int most = 0;
+    // a sequence's tiles at level L or above
+    auto part = [&](int tiles, int level, int L) {
+        const int y = level - L + 1;
+        return y < 0 ? 0 : y < tiles ? y : tiles;
+    };
+    int sum[NC];
+#pragma unroll
+    for (int k = 0; k < NC; ++k)
+        sum[k] = 0;
+    auto add = [&](int tiles, int level) {
+#pragma unroll
+        for (int k = 0; k < NC - 1; ++k)
+            sum[k] += part(tiles, level, p.class_of[k]);
+        sum[NC - 1] += tiles;
+    };
 #pragma unroll
     for (int c = 0; c < KEPT; ++c) {
         nqt[c] = top[c] = 0;
-        if (c < nch)
+        if (c < nch) {
             load(c, nqt[c], top[c]);
-        most = most > top[c] ? most : top[c];
+            add(nqt[c], top[c]);
+        }
     }
     for (int c = KEPT; c < nch; ++c) {
         int a, b;
         load(c, a, b);
-        most = most > b ? most : b;
+        add(a, b);
     }
-    auto at_or_above = [&](int L) {
-        auto part = [&](int tiles, int level) {
-            const int x = level - L + 1;
-            return x < 0 ? 0 : x < tiles ? x : tiles;
-        };
-        int sum = 0;
+    wave_scan(sum);
+    int from = 0, lower = 1, upper = 0x7fffffff;  // tiles before the class, its lowest level and that of the class before
+    bool found = false;
 #pragma unroll
-        for (int c = 0; c < KEPT; ++c)
-            sum += part(nqt[c], top[c]);
-        for (int c = KEPT; c < nch; ++c) {
-            int a, b;
-            load(c, a, b);
-            sum += part(a, b);
+    for (int k = 0; k < NC; ++k) {
+        const int end = __builtin_amdgcn_readlane(sum[k], 63);
+        if (!found && i >= end) {
+            from = end;
+            if (k < NC - 1)
+                upper = p.class_of[k];
+        } else if (!found) {
+            found = true;
+            lower = k < NC - 1 ? p.class_of[k] : 1;
         }
-        return wave_sum(sum);
-    };
-    t.qt = -1;
-    if (at_or_above(1) <= i)
-        return t;
-    int lo = 1, hi = 1;
-    while (__builtin_amdgcn_ballot_w64(most > hi) != 0)  // the highest level, within a factor of two
-        hi *= 2;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (at_or_above(mid) > i)
-            lo = mid;
-        else
-            hi = mid - 1;
     }
-    int rank = i - at_or_above(lo + 1);  // among the sequences that have a tile at this level
-    for (int c = 0; c < nch; ++c) {
-        int a, b;
-        if (c < KEPT) {
-            a = c == 0 ? nqt[0] : c == 1 ? nqt[1] : c == 2 ? nqt[2] : nqt[3];
-            b = c == 0 ? top[0] : c == 1 ? top[1] : c == 2 ? top[2] : top[3];
+    if (!found)
+        return t;  // the grid is an upper bound
+    int rank = i - from;
+    auto pick = [&](int c, int tiles, int level) {
+        const int before = upper == 0x7fffffff ? 0 : part(tiles, level, upper);
+        const int m = part(tiles, level, lower) - before;
+        const int incl = wave_scan(m);
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > rank);
+        if (mask == 0) {
+            rank -= __builtin_amdgcn_readlane(incl, 63);
+            return false;
+        }
+        const int src = __builtin_ctzll(mask);
+        t.qt = __builtin_amdgcn_readlane(tiles - 1 - before + incl - m, src) - rank;
+        if (c == 0) {
+            t.q0 = __builtin_amdgcn_readlane(first.q0, src);
+            t.k0 = __builtin_amdgcn_readlane(first.k0, src);
+            t.Sq = __builtin_amdgcn_readlane(first.Sq, src);
+            t.Sk = __builtin_amdgcn_readlane(first.Sk, src);
         } else {
-            load(c, a, b);
+            const PackedSeq s = packed_seq(p, c * 64 + src);
+            t.q0 = __builtin_amdgcn_readfirstlane(s.q0);
+            t.k0 = __builtin_amdgcn_readfirstlane(s.k0);
+            t.Sq = __builtin_amdgcn_readfirstlane(s.Sq);
+            t.Sk = __builtin_amdgcn_readfirstlane(s.Sk);
         }
-        const bool has = b >= lo && b - a < lo;
-        const unsigned long long mask = __builtin_amdgcn_ballot_w64(has);
-        const int count = __builtin_popcountll(mask);
-        if (rank >= count) {
-            rank -= count;
-            continue;
-        }
-        const int before = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0u));
-        const int src = __builtin_ctzll(__builtin_amdgcn_ballot_w64(has && before == rank));
-        t.qt = __builtin_amdgcn_readlane(a, src) - 1 - (__builtin_amdgcn_readlane(b, src) - lo);
-        const PackedSeq s = packed_seq(p, c * 64 + src);
-        t.q0 = __builtin_amdgcn_readfirstlane(s.q0);
-        t.k0 = __builtin_amdgcn_readfirstlane(s.k0);
-        t.Sq = __builtin_amdgcn_readfirstlane(s.Sq);
-        t.Sk = __builtin_amdgcn_readfirstlane(s.Sk);
-        break;
+        t.rows = t.Sq * p.g;
+        return true;
+    };
+#pragma unroll
+    for (int c = 0; c < KEPT; ++c)
+        if (c < nch && pick(c, nqt[c], top[c]))
+            return t;
+    for (int c = KEPT; c < nch; ++c) {
+        int a, b;
+        load(c, a, b);
+        if (pick(c, a, b))
+            return t;
     }
     return t;
 }
 
-// Rows that see no key: O is 0 and lse is -inf.  Rows first .. first + count of the packed tensors, by a whole work-group.
+// Rows that see no key: O is 0 and lse is -inf.  Rows first .. first + count of a tile's sequence, by a whole work-group.
 template <int OUTB>
-__device__ __forceinline__ void packed_empty_rows(const PackedParams& p, int hq, int first, int count, int tid, int threads)
+__device__ __forceinline__ void packed_empty_rows(const PackedParams& p, const PackedTile& t, int first, int count, int tid, int threads)
 {
     const int pieces = p.cpr * 2;  // four values each
-    unsigned char* const o = (unsigned char*)p.o + (long long)first * p.o_rs + hq * p.o_hs;
     for (int x = tid; x < count * pieces; x += threads) {
-        unsigned char* const at = o + (long long)(x / pieces) * p.o_rs + x % pieces * (4 * OUTB);
+        const int r = first + x / pieces;
+        unsigned char* const at = (unsigned char*)p.o + (long long)(t.q0 + r / p.g) * p.o_rs + (t.hk * p.g + r % p.g) * p.o_hs + x % pieces * (4 * OUTB);
         if constexpr (OUTB == 2)
             *(i32x2_t*)at = i32x2_t{0, 0};
         else
             *(f32x4_t*)at = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (p.lse != nullptr && x % pieces == 0)
+            p.lse[(size_t)(t.hk * p.g + r % p.g) * p.Tq + t.q0 + r / p.g] = -INFINITY;
     }
-    if (p.lse != nullptr)
-        for (int x = tid; x < count; x += threads)
-            p.lse[(size_t)hq * p.Tq + first + x] = -INFINITY;
 }
 
 }  // namespace naut_k
