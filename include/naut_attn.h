@@ -289,7 +289,7 @@ int naut_kv4_scale_bytes(int D);
 /*
  * Writes T rows of k and v ([T][Hkv][D], in_dtype NAUT_BF16 or NAUT_F16) into the cache: row t goes to position slots[t] % S
  * of sequence slots[t] / S; a slot below 0 or from B*S on is skipped, as the padding of a batch is.  slots is DEVICE memory, T
- * int; no position may occur twice in one call.  The scale of a block is the least power of two 2^e with max|x| < 7 * 2^e (at
+ * int (T at most 2^30, 0 does nothing); no position may occur twice in one call.  The scale of a block is the least power of two 2^e with max|x| < 7 * 2^e (at
  * which the largest value does not round past 6), but at most 2^125 (NAUT_F16: 2^13, so that every value is finite in the type) and at least 2^-126;
  * codes are rounded to nearest, ties to the even code, and saturate.  Values must be finite.  `st` gives the head and
  * sequence (row) strides of k and v in elements, non-negative multiples of 8 (NULL = contiguous; its other members are not looked at).

@@ -99,7 +99,8 @@ def test_row_refusals():
         assert call(k=A + 8) == call(slots=A + 2) == nb.NAUT_ERR_ALIGN
         row = lambda k_h, k_s, v_h, v_s: (0, 0, 0, 0, k_h, k_s, 0, v_h, v_s, 0, 0, 0)
         assert call(st=row(64, 132, 64, 128)) == call(st=row(64, 128, -64, 128)) == nb.NAUT_ERR_ALIGN
-        assert store(cache(B=1, S=1 << 30), f=f, T=1 << 30) == nb.NAUT_ERR_UNSUPPORTED
+        assert call(T=(1 << 30) + 1) == nb.NAUT_ERR_UNSUPPORTED
+        assert store(cache(Hkv=1 << 12), f=f, T=1 << 30) == nb.NAUT_ERR_UNSUPPORTED              # more work-groups than a grid has
     assert store(cache(), f="naut_kv4_load", st=row(0, 128, 64, 128)) == nb.NAUT_ERR_ALIGN     # rows written to the same place
     assert store(cache(), f="naut_kv4_load", st=row(64, 56, 64, 128)) == nb.NAUT_ERR_SHAPE
     for c in (cache(c=(6400, 0, 32)), cache(c=(0, 3200, 32)), cache(s=(400, 0, 2)), cache(s=(0, 200, 2))):
