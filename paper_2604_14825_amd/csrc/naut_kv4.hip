@@ -280,7 +280,7 @@ int launched()
 //   K goes from memory into registers: a lane's 16 bytes of codes are one block of 32 values of one key, four conversions make
 // eight of them an A operand, and Q is loaded in the order that this gives the contraction.  V's codes come in the same
 // way, are converted, and pass through the wavefront's own LDS as 16-bit rows to be read transposed.
-constexpr int KV_BLK = 32;    // keys per block
+constexpr int KV_SHIFT = 5, KV_BLK = 1 << KV_SHIFT;  // keys per block
 constexpr int KV_TARGET = 256;  // work-groups that the plan aims at: one to a CU, of eight wavefronts
 constexpr int MRG_WAVES = 4;
 
@@ -326,8 +326,16 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
 {
     if (x >= p.P)
         return false;  // the grid is rounded up
+    if (p.P == p.B) {  // short caches, or many: a part each
+        out->b = x;
+        out->split = out->first = out->begin = 0;
+        out->nsplit = 1;
+        out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, x));
+        out->end = ((out->len - 1) >> KV_SHIFT) + 1;
+        return true;
+    }
     const int nch = (p.B + 63) >> 6;
-    auto blocks = [&](int c) { return c * 64 + lane < p.B ? (kv4_len(p, c * 64 + lane) + KV_BLK - 1) / KV_BLK : -1; };
+    auto blocks = [&](int c) { return c * 64 + lane < p.B ? ((kv4_len(p, c * 64 + lane) - 1) >> KV_SHIFT) + 1 : -1; };
     const int mine = blocks(0);  // the first 64's, kept
     auto of = [&](int c) { return c == 0 ? mine : blocks(c); };
     // Parts of a sequence of n blocks.  Need not be the exact quotient: its blocks are dealt out evenly over whatever it is.
@@ -349,7 +357,7 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
     int L = (total + p.P - 1) / p.P;
     L = L > p.least ? L : p.least;
     if (count(L) > p.P) {
-        const int longest = (p.S + KV_BLK - 1) / KV_BLK + 1;  // a part each
+        const int longest = ((p.S - 1) >> KV_SHIFT) + 2;  // a part each
         int lo = L, hi = p.P > p.B ? total / (p.P - p.B) + 1 : longest;
         hi = hi < longest && count(hi) <= p.P ? hi : longest;
         while (hi - lo > (lo >> 4) + 1) {
@@ -434,7 +442,10 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
 {
     using X = Mx<DT>;
     constexpr int NW = kv4_waves(D, RT);
-    constexpr int KS = D / 32;             // words of codes, and MFMAs, per key tile
+    // A lane's codes of a block: 16 bytes, one block of 32 values, of one key at a time.  At D >= 128 the four lane groups hold
+    // the blocks of the same 16 keys (SETS = 2 of them to a block of keys), at D = 64 two groups those of either key tile.
+    constexpr int SETS = D == 64 ? 1 : 2;
+    constexpr int KW = D == 64 ? 4 : D / 32;  // words of codes, and MFMAs, per set
     constexpr int DT16 = D / 16;           // 16-row tiles of O^T
     constexpr int VROW = v4_row(D), VB = KV_BLK * VROW;  // a block of V in LDS
     constexpr int OB = RT * 16 * D * 4;    // a wavefront's O
@@ -456,16 +467,19 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     const unsigned char* const cg[2] = {p.codes[0] + b * p.c_b + hk * p.c_h, p.codes[1] + b * p.c_b + hk * p.c_h};
     const unsigned char* const sg[2] = {p.scales[0] + b * p.s_b + hk * p.s_h, p.scales[1] + b * p.s_b + hk * p.s_h};
 
-    // A lane's words of a key's row: word ks holds the values dim(ks) .. + 8, which is the contraction order of MFMA ks.
-    auto dim = [&](int ks) { return D == 64 ? 16 * g4 + 8 * ks : 32 * (4 * (ks >> 2) + g4) + 8 * (ks & 3); };
+    const int key_of = D == 64 ? 16 * (g4 >> 1) + l16 : l16;  // the key of set 0, in the block
+    // Word ks holds the values dim(ks) .. + 8 of the key's row, which is the contraction order of MFMA ks.
+    auto dim = [&](int ks) { return D == 64 ? 32 * (g4 & 1) + 8 * ks : 32 * (4 * (ks >> 2) + g4) + 8 * (ks & 3); };
     // the block of a lane's chunk j (D = 256 has two), a real one also where the head is narrower
     auto blk_of = [&](int j) {
-        const int x = D == 64 ? g4 >> 1 : 4 * j + g4;
+        const int x = D == 64 ? g4 & 1 : 4 * j + g4;
         return x < p.nb ? x : p.nb - 1;
     };
     constexpr int CH = D == 256 ? 2 : 1;   // chunks per lane and key
 
-    i32x4_t qf[RT][KS];
+    // D = 64: one copy of Q for each key tile, zero in the lanes that hold the other's keys (twice the MFMAs, half the loads)
+    constexpr int QT = D == 64 ? 2 : 1;
+    i32x4_t qf[RT][QT][KW];
     int lim[RT];  // last key that the lane's row sees
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
@@ -473,51 +487,74 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
         const unsigned char* const qr = (const unsigned char*)p.q + b * p.q_bs + (hk * g + r / p.Sq) * p.q_hs + (long long)(r % p.Sq) * p.q_rs;
         lim[rt] = p.causal ? len - p.Sq + r % p.Sq : len - 1;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-            qf[rt][ks] = dim(ks) < p.nb * MX ? *(const i32x4_t*)(qr + dim(ks) * 2) : i32x4_t{0, 0, 0, 0};
+        for (int ks = 0; ks < KW; ++ks) {
+            const i32x4_t x = dim(ks) < p.nb * MX ? *(const i32x4_t*)(qr + dim(ks) * 2) : i32x4_t{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < QT; ++t)
+                qf[rt][t][ks] = QT == 1 || g4 >> 1 == t ? x : i32x4_t{0, 0, 0, 0};
+        }
     }
 
-    // Codes and scale bytes of the lane's keys of a block, of K or of V.  The next block's are requested into the same registers
-    // as soon as this block's have been converted.
+    // Codes of the lane's keys of a block, of K or of V.  The next block's are requested into the same registers as soon as this
+    // block's have been converted.
     struct Block {
-        int w[2][KS];   // [key tile][word]
-        int s[2][CH];
+        int w[SETS][KW];
     };
     const int c_s = (int)p.c_s, s_s = (int)p.s_s;
     auto load = [&](Block& x, int kv, int blk) {
         const int left = len - 1 - blk * KV_BLK;  // the ragged last block reads its last key again
         const unsigned char* const cb = cg[kv] + (long long)blk * (KV_BLK * (long long)c_s);
-        const unsigned char* const sb = sg[kv] + (long long)blk * (KV_BLK * (long long)s_s);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            int key = t * 16 + l16;
+        for (int t = 0; t < SETS; ++t) {
+            int key = t * 16 + key_of;
             key = key < left ? key : left;
 #pragma unroll
             for (int j = 0; j < CH; ++j) {
-                const unsigned co = (unsigned)(key * c_s + (D == 64 ? (g4 * 8 < p.nb * 16 ? g4 * 8 : 0) : blk_of(j) * 16));
-                if constexpr (D == 64) {
-                    const i32x2_t y = *(const i32x2_t*)(cb + co);
-                    x.w[t][0] = y.x;
-                    x.w[t][1] = y.y;
-                } else {
-                    const i32x4_t y = *(const i32x4_t*)(cb + co);
+                const i32x4_t y = *(const i32x4_t*)(cb + (unsigned)(key * c_s + blk_of(j) * 16));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        x.w[t][4 * j + i] = y[i];
-                }
-                x.s[t][j] = sb[(unsigned)(key * s_s + blk_of(j))];
+                for (int i = 0; i < 4; ++i)
+                    x.w[t][4 * j + i] = y[i];
             }
         }
     };
+    // The scales of a block's 32 keys of K and of V, a key's row of them to a lane (K's in the lower half of the lanes): one load
+    // that touches every line once.  (A byte to a lane straight from memory is four loads, and where the rows of heads lie side by
+    // side they cost as much as the codes: 8 sequence-major caches of 16384 keys, 8 heads, D = 128 37.2 us for 28.4.)  Each
+    // lane then fetches the words of its keys.
+    int sw[CH];
+    const unsigned char* const sl = lane < 32 ? sg[0] : sg[1];
+    auto load_scales = [&](int blk) {
+        const int left = len - 1 - blk * KV_BLK, key = (lane & 31) < left ? lane & 31 : left;
+        const unsigned char* const at = sl + (long long)(blk * KV_BLK + key) * s_s;
+        if constexpr (D == 64) {
+            sw[0] = *(const unsigned short*)at;
+        } else if constexpr (D == 128) {
+            sw[0] = *(const int*)at;
+        } else {
+            const i32x2_t y = *(const i32x2_t*)at;
+            sw[0] = y.x;
+            sw[CH - 1] = y.y;
+        }
+    };
+    float sc[2][SETS][CH];  // of K, V
+    auto spread_scales = [&](int kv) {
+#pragma unroll
+        for (int t = 0; t < SETS; ++t)
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+                const int row = __builtin_amdgcn_ds_bpermute((kv * 32 + t * 16 + key_of) * 4, sw[j]);
+                sc[kv][t][j] = mx_scale(X::scale_of(row >> ((blk_of(j) & 3) * 8) & 0xff));
+            }
+    };
     // eight values of word ks
-    auto values = [&](const Block& x, int t, int ks) -> i32x4_t {
-        const float s = mx_scale(X::scale_of(x.s[t][CH == 1 ? 0 : ks >> 2]));
+    auto values = [&](const Block& x, int kv, int t, int ks) -> i32x4_t {
+        const float s = sc[kv][t][CH == 1 ? 0 : ks >> 2];
         const int w = x.w[t][ks];
         return i32x4_t{X::template decode<0>(w, s), X::template decode<1>(w, s), X::template decode<2>(w, s), X::template decode<3>(w, s)};
     };
 
-    // where the lane writes its values of V's key l16, and reads keys 4 g4 .. 4 g4 + 3 of 16 columns transposed
-    unsigned char* const v_write = smem + wave * REGION + l16 * VROW + dim(0) * 2;
+    // where the lane writes its values of V's key, and reads keys 4 g4 .. 4 g4 + 3 of 16 columns transposed
+    unsigned char* const v_write = smem + wave * REGION + key_of * VROW + dim(0) * 2;
     const unsigned char* const v_read = smem + wave * REGION + (4 * g4 + (l16 >> 2)) * VROW + (l16 & 3) * 8;
     f32x4_t oacc[RT][DT16];
     float m_run[RT], l_run[RT];  // reference maximum (log2 units, the lowest value there is at first), the lane's share of the sum
@@ -533,32 +570,37 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     Block kx, vx;
     int blk = sp.begin + wave;
     if (blk < sp.end) {
+        load_scales(blk);
         load(kx, 0, blk);
         load(vx, 1, blk);
     }
     for (; blk < sp.end; blk += NW) {
         const int nxt = blk + NW < sp.end ? blk + NW : blk;  // the last one's loads are for nobody, and cost less than a branch
+        spread_scales(0);
         f32x4_t s[RT][2];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int rt = 0; rt < RT; ++rt)
+            s[rt][0] = s[rt][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-                s[rt][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < SETS; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const i32x4_t kf = values(kx, t, ks);
+            for (int ks = 0; ks < KW; ++ks) {
+                const i32x4_t kf = values(kx, 0, t, ks);
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt)
-                    s[rt][t] = X::mfma(kf, qf[rt][ks], s[rt][t]);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+                        s[rt][t + u] = X::mfma(kf, qf[rt][u][ks], s[rt][t + u]);
             }
-        }
+        spread_scales(1);
+        load_scales(nxt);
         load(kx, 0, nxt);
         // V to LDS, as rows of 16-bit values
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < SETS; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                *(i32x4_t*)(v_write + t * 16 * VROW + (ks >> 2) * 256 + (ks & 3) * 16) = values(vx, t, ks);
+            for (int ks = 0; ks < KW; ++ks)
+                *(i32x4_t*)(v_write + t * 16 * VROW + (ks >> 2) * 256 + (ks & 3) * 16) = values(vx, 1, t, ks);
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -664,12 +706,12 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     }
 }
 
-// One work-group per query row: the splits of its sequence, where there are several.  Wavefront w takes splits w, w + 4, ..., eight
-// of them at a time; lanes run over D.
+// One work-group per query row: the splits of its sequence, where there are several.  Wavefront w takes splits w, w + 4, ..., up
+// to eight of them at a time; lanes run over D.
 template <int D, int DT>
 __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(const Kv4Params p)
 {
-    constexpr int EPT = D / 64, BATCH = 8;
+    constexpr int EPT = D / 64;
     typedef float fe_t __attribute__((ext_vector_type(EPT)));
     __shared__ float red_m[MRG_WAVES], red_l[MRG_WAVES];
     __shared__ __attribute__((aligned(16))) float red_o[MRG_WAVES][D];
@@ -689,32 +731,41 @@ __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(c
     const float* const ws_o = p.ws + (part0 * p.rows + r) * D;
     fe_t acc = (fe_t)(0.f);
     float M = -FLT_MAX, L = 0.f;
-    for (int s0 = wave; s0 < nsplit; s0 += MRG_WAVES * BATCH) {
-        float m[BATCH], l[BATCH];
-        fe_t x[BATCH];
+    auto gather = [&](auto BC) {
+        constexpr int BATCH = decltype(BC)::value;
+        for (int s0 = wave; s0 < nsplit; s0 += MRG_WAVES * BATCH) {
+            float m[BATCH], l[BATCH];
+            fe_t x[BATCH];
 #pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const int s = s0 + u * MRG_WAVES;
-            const size_t sc = s < nsplit ? s : s0;  // past the end: repeats a split, not added
-            m[u] = ws_m[sc * p.rows];
-            l[u] = ws_l[sc * p.rows];
-            x[u] = *(const fe_t*)(ws_o + sc * p.rows * D + lane * EPT);
+            for (int u = 0; u < BATCH; ++u) {
+                const int s = s0 + u * MRG_WAVES;
+                const size_t sc = s < nsplit ? s : s0;  // past the end: repeats a split, not added
+                m[u] = ws_m[sc * p.rows];
+                l[u] = ws_l[sc * p.rows];
+                x[u] = *(const fe_t*)(ws_o + sc * p.rows * D + lane * EPT);
+            }
+            float m_new = M;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u)
+                m_new = fmaxf(m_new, m[u]);
+            const float alpha = __builtin_amdgcn_exp2f(M - m_new);
+            M = m_new;
+            L *= alpha;
+            acc *= alpha;
+#pragma unroll
+            for (int u = 0; u < BATCH; ++u) {
+                const float f = s0 + u * MRG_WAVES < nsplit ? __builtin_amdgcn_exp2f(m[u] - M) : 0.f;
+                L += f * l[u];
+                acc += f * x[u];
+            }
         }
-        float m_new = M;
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u)
-            m_new = fmaxf(m_new, m[u]);
-        const float alpha = __builtin_amdgcn_exp2f(M - m_new);
-        M = m_new;
-        L *= alpha;
-        acc *= alpha;
-#pragma unroll
-        for (int u = 0; u < BATCH; ++u) {
-            const float f = s0 + u * MRG_WAVES < nsplit ? __builtin_amdgcn_exp2f(m[u] - M) : 0.f;
-            L += f * l[u];
-            acc += f * x[u];
-        }
-    }
+    };
+    if (nsplit <= MRG_WAVES)
+        gather(std::integral_constant<int, 1>{});
+    else if (nsplit <= 2 * MRG_WAVES)
+        gather(std::integral_constant<int, 2>{});
+    else
+        gather(std::integral_constant<int, 8>{});
     *(fe_t*)&red_o[wave][lane * EPT] = acc;
     if (lane == 0) {
         red_m[wave] = M;
