@@ -281,6 +281,7 @@ int launched()
 // eight of them an A operand, and Q is loaded in the order that this gives the contraction.  V's codes come in the same
 // way, are converted, and pass through the wavefront's own LDS as 16-bit rows to be read transposed.
 constexpr int KV_SHIFT = 5, KV_BLK = 1 << KV_SHIFT;  // keys per block
+constexpr int KV_FINER = 2;     // how much finer it cuts more sequences than fill the chip
 constexpr int KV_TARGET = 256;  // work-groups that the plan aims at: one to a CU, of eight wavefronts
 constexpr int MRG_WAVES = 4;
 
@@ -296,7 +297,8 @@ struct Kv4Params {
     int R;            // query rows per (sequence, K/V head)
     int rows;         // of a chunk of them, a multiple of 16
     int nchunks;
-    int P;            // splits of all sequences together, at most (the grid)
+    int aim;          // splits of all sequences together that fill the chip
+    int P;            // and at most: KV_FINER aim + B, or B where every sequence is one split (the grid)
     int least;        // blocks per split, at least
     int causal;
     float c;          // scale * log2(e), > 0
@@ -318,14 +320,16 @@ struct Kv4Split {
 };
 
 // Which part of which sequence split x is: every sequence is cut into equal parts of about L blocks (an empty one is one
-// part), for an L at which they are no more than P.  The mean, total / P, is the least that can do and does where the
-// lengths are alike; total / (P - B) always does, as no sequence has more than a part beyond its share.  Between them by halving, to a
-// sixteenth: a longer search costs more than the shorter splits give (with a full one over the 16 ragged sequences of 24.7 MB
-// of keys and values the call took 1.7 us longer).  64 sequences at a time, one to a lane.
+// part).  L is the mean, total / aim, where that makes no more than `aim` parts, as it does for lengths that are alike; or up to twice
+// the mean if that keeps them to `aim`, found by halving to a sixteenth (a further round of work-groups costs more than longer parts,
+// a longer search more than the shorter parts give); or, with many sequences or one that is most of the batch, half the mean
+// (at most 2 aim + B parts).  32/8 heads, D = 128, us with L = total / max(aim, B) always, the mean, half and a quarter of it: one of
+// 30000 among 47 of 100 keys 115 / 17.5 / 18.1 / 22.1, 100 of 1 to 8192 103 / 108 / 98 / 91, 64 of 5000 60.5 / 64.1 / 63.9 / 68.1.
+// 64 sequences at a time, one to a lane.
 __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, Kv4Split* out)
 {
     if (x >= p.P)
-        return false;  // the grid is rounded up
+        return false;  // the grid is rounded up to eights
     if (p.P == p.B) {  // short caches, or many: a part each
         out->b = x;
         out->split = out->first = out->begin = 0;
@@ -354,20 +358,23 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
     for (int c = 0; c < nch; ++c)
         total += of(c) > 0 ? of(c) : 0;
     total = wave_sum(total);
-    int L = (total + p.P - 1) / p.P;
+    int L = (total + p.aim - 1) / p.aim;
     L = L > p.least ? L : p.least;
-    if (count(L) > p.P) {
-        const int longest = ((p.S - 1) >> KV_SHIFT) + 2;  // a part each
-        int lo = L, hi = p.P > p.B ? total / (p.P - p.B) + 1 : longest;
-        hi = hi < longest && count(hi) <= p.P ? hi : longest;
-        while (hi - lo > (lo >> 4) + 1) {
-            const int mid = (lo + hi) >> 1;
-            if (count(mid) <= p.P)
-                hi = mid;
-            else
-                lo = mid;
+    if (count(L) > p.aim) {
+        if (count(2 * L) <= p.aim) {
+            int lo = L, hi = 2 * L;
+            while (hi - lo > (lo >> 4) + 1) {
+                const int mid = (lo + hi) >> 1;
+                if (count(mid) <= p.aim)
+                    hi = mid;
+                else
+                    lo = mid;
+            }
+            L = hi;
+        } else {
+            L = (total + p.aim * KV_FINER - 1) / (p.aim * KV_FINER);
+            L = L > p.least ? L : p.least;
         }
-        L = hi;
     }
     const float rcp = __builtin_amdgcn_rcpf((float)L);
     int before = 0;
@@ -456,9 +463,15 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g4 = lane >> 4;
-    const int chunk = blockIdx.y, hk = blockIdx.z;
+    // Work-groups are dealt to the XCDs by linear id mod 8.  Eight splits of every chunk and K/V head are neighbours, so that a
+    // split of all of them is on one XCD, whose L2 serves the chunks from one read and the heads of a sequence-major cache from
+    // whole lines; a number of splits that eight does not divide would leave XCDs idle, and goes one by one.  The splits that
+    // no sequence has come last either way: ahead of others they would make room for two work-groups on one CU
+    // and none on another (8 caches of 16384 keys 27.5 us for 37.2).
+    const int eight = p.aim & 7 ? 0 : 3, y = blockIdx.x >> eight, x_of = (blockIdx.y << eight) + (blockIdx.x & ((1 << eight) - 1));
+    const int chunk = p.nchunks == 1 ? 0 : y / p.Hkv, hk = y - chunk * p.Hkv;
     Kv4Split sp;
-    if (!kv4_split(p, blockIdx.x, lane, &sp))
+    if (!kv4_split(p, x_of, lane, &sp))
         return;
     const int b = sp.b, len = sp.len;
     const int g = p.Hq / p.Hkv;
@@ -670,7 +683,7 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     }
     __syncthreads();
     const int rows = p.R - row0 < p.rows ? p.R - row0 : p.rows;
-    const int part = (hk * p.nchunks + chunk) * p.P + blockIdx.x;
+    const int part = (hk * p.nchunks + chunk) * p.P + x_of;
     const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
     float* const ws_m = p.ws + nparts * p.rows * D;
     float* const ws_l = ws_m + nparts * p.rows;
@@ -798,16 +811,19 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
     const long long R = (long long)(Hq / Hkv) * Sq;
     const int rows = R <= 16 ? 16 : 32;
     const long long nchunks = (R + rows - 1) / rows;
-    if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535)
+    if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535 - KV_FINER * KV_TARGET || nchunks * Hkv > 1 << 24)
         return false;
     const long long nblk = (S + KV_BLK - 1LL) / KV_BLK;
     const long long least = kv4_waves(kv4_width(D), rows / 16);  // a block for every wavefront
-    long long P = KV_TARGET / (Hkv * nchunks);
-    const long long each = nblk <= 2 * least ? 1 : (nblk + least - 1) / least;  // splits that a full sequence can have
-    P = P < B ? B : P < B * each ? P : B * each;
+    const long long aim = KV_TARGET / (Hkv * nchunks) > 1 ? KV_TARGET / (Hkv * nchunks) : 1;
+    // A part each, and so no merge: where a whole cache is two blocks for every wavefront, or eight and there are enough of them
+    // (what a merge costs, 4 us, is what the longest can be behind the others).
+    const bool one = nblk <= 2 * least || (B >= aim && nblk <= 8 * least);
+    const long long P = one ? B : aim * KV_FINER + B;
     p->R = (int)R;
     p->rows = rows;
     p->nchunks = (int)nchunks;
+    p->aim = (int)aim;
     p->P = (int)P;
     p->least = (int)least;
     *bytes = P > B ? ((size_t)Hkv * nchunks * P * rows * (kv4_width(D) + 2) * sizeof(float) + (size_t)B * 2 * sizeof(int) + 15) / 16 * 16 : 16;
@@ -817,9 +833,8 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
 template <int D, int DT>
 int launch_kv4(const Kv4Params& p, hipStream_t stream)
 {
-    // Work-groups are dealt to the XCDs by linear id mod 8: rounded up to eights, the same split of every K/V head and chunk is on
-    // one XCD, whose L2 serves the chunks from one read and the heads of a sequence-major cache from whole lines.
-    const dim3 grid((unsigned)(p.P + 7) / 8 * 8, (unsigned)p.nchunks, (unsigned)p.Hkv);
+    const unsigned eight = p.aim & 7 ? 1 : 8;
+    const dim3 grid((unsigned)(p.Hkv * p.nchunks) * eight, ((unsigned)p.P + eight - 1) / eight);
     if (p.rows == 16)
         hipLaunchKernelGGL((naut_decode_kv4_kernel<D, DT, 1>), grid, dim3(kv4_waves(D, 1) * 64), 0, stream, p);
     else

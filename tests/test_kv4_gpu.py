@@ -194,6 +194,15 @@ def test_many_sequences(B):
 
 def test_one_long_sequence_among_short_ones():
     run(8, 2, 1, 30000, 128, [3, 30000, 0, 17, 1, 2900], seed=6)
+    run(6, 3, 1, 30000, 64, [30000] + [5] * 40, seed=6)     # three K/V heads: a number of splits that eight does not divide
+    run(10, 5, 2, 12000, 128, [12000, 300, 11000], seed=6)
+
+
+def test_more_sequences_than_fill_the_chip():
+    """And too long for a part each: the mean is cut in halves."""
+    rng = np.random.default_rng(300)
+    run(2, 1, 1, 3000, 64, [int(x) for x in rng.integers(0, 3001, 300)], seed=14)
+    run(4, 4, 1, 2500, 128, [2500] * 70, seed=14)
 
 
 @pytest.mark.parametrize("D", [64, 128, 256])
