@@ -257,7 +257,7 @@ size_t naut_attn_decode_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * whatever they hold.  A pair of offsets that falls, is negative or passes Tq or Tk makes its sequence empty.
  * `st` gives the head and sequence (row) strides in elements, by the rules of naut_attn_fwd_strided; the batch strides are not
  * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Hq/Hkv at most 1024, Tq and Tk times that
- * at most 2^30, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
+ * at most 2^30, Hkv at most 65535, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
  */
 int naut_attn_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_q,
                          const int* cu_k, int n, int Tq, int Tk, int Hq, int Hkv, int D, int causal, float scale,
@@ -289,7 +289,7 @@ int naut_kv4_scale_bytes(int D);
 /*
  * Writes T rows of k and v ([T][Hkv][D], in_dtype NAUT_BF16 or NAUT_F16) into the cache: row t goes to position slots[t] % S
  * of sequence slots[t] / S; a slot below 0 or from B*S on is skipped, as the padding of a batch is.  slots is DEVICE memory, T
- * int (T at most 2^30, 0 does nothing); no position may occur twice in one call.  The scale of a block is the least power of two 2^e with max|x| < 7 * 2^e (at
+ * int (0 does nothing; at most 2^30, and about 2^34 / D rows of heads); no position may occur twice in one call.  The scale of a block is the least power of two 2^e with max|x| < 7 * 2^e (at
  * which the largest value does not round past 6), but at most 2^125 (NAUT_F16: 2^13, so that every value is finite in the type) and at least 2^-126;
  * codes are rounded to nearest, ties to the even code, and saturate.  Values must be finite.  `st` gives the head and
  * sequence (row) strides of k and v in elements, non-negative multiples of 8 (NULL = contiguous; its other members are not looked at).

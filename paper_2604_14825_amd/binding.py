@@ -543,7 +543,7 @@ def _call(device, f, *args):
 def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float, stream=None):
     """Attention forward on packed sequences of different lengths.
 
-    q,o [Tq,Hq,D]; k,v [Tk,Hkv,D] (the last axis contiguous, any head and row strides); lse contiguous fp32 [Hq,Tq] or
+    q,o [Tq,Hq,D]; k,v [Tk,Hkv,D] (the last axis contiguous, head and row strides of whole 16 bytes); lse contiguous fp32 [Hq,Tq] or
     None; cu_q, cu_k contiguous int32 device tensors [n+1], the offsets of the n sequences' rows (they may be one tensor).
     The queries of a sequence are the last positions of its keys.  Rows of no sequence are left as they are, a row that
     sees no key gets o = 0 and lse = -inf.  Enqueues on `stream` and returns; the lengths are read on the GPU."""
@@ -571,7 +571,7 @@ def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float
                                       0, o.stride(1), o.stride(0)))
     _call(device, lib().naut_attn_fwd_packed, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(),
           None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), n, Tq, Tk, Hq, Hkv, D, 1 if causal else 0,
-          scale, _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o), st)
+          float(scale), _stream_ptr(stream, q), _torch_dtype_code(q), _torch_dtype_code(o), st)
 
 
 def kv4_scale_bytes(D: int) -> int:
@@ -673,7 +673,7 @@ def naut_attn_decode_kv4(q, o, lse, cache, lens, causal: bool, scale: float, wor
             raise ValueError("lens must be a contiguous int32 device tensor [B]")
         lens_ptr = lens.data_ptr()
     _call(device, lib().naut_attn_decode_kv4, q.data_ptr(), o.data_ptr(), lse_ptr, cache.ref, lens_ptr, Hq, Sq, 1 if causal else 0,
-          scale, workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, q), _torch_dtype_code(q),
+          float(scale), workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_ptr(stream, q), _torch_dtype_code(q),
           _torch_dtype_code(o), st)
 
 

@@ -236,7 +236,7 @@ int rows_of(const void* k, const void* v, const naut_kv4_cache* c, const int* sl
         return fail(NAUT_ERR_SHAPE, "a cache that is stored to cannot have heads or sequences in the same place (stride 0)");
     if (load && (st->k_s < c->D || st->v_s < c->D))
         return fail(NAUT_ERR_SHAPE, "a sequence stride is smaller than D: rows would overlap");
-    if (T > 1 << 30 || ((long long)T / (2048 / c->D) + 1) * c->Hkv > 0x7fffffffLL)
+    if (T > 1 << 30 || ((long long)T / (2048 / c->D) + 1) * c->Hkv > 1 << 23)  // 2^31 threads
         return fail(NAUT_ERR_UNSUPPORTED, "too many rows for one call");
     p->codes[0] = (unsigned char*)c->k_codes;
     p->codes[1] = (unsigned char*)c->v_codes;
@@ -811,7 +811,7 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
     const long long R = (long long)(Hq / Hkv) * Sq;
     const int rows = R <= 16 ? 16 : 32;
     const long long nchunks = (R + rows - 1) / rows;
-    if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535 - KV_FINER * KV_TARGET || nchunks * Hkv > 1 << 24)
+    if (R > 0x7fffffffLL / 4 || nchunks > 65535 || Hkv > 65535 || B > 65535 - KV_FINER * KV_TARGET || nchunks * Hkv > 1 << 22)  // 2^31 threads
         return false;
     const long long nblk = (S + KV_BLK - 1LL) / KV_BLK;
     const long long least = kv4_waves(kv4_width(D), rows / 16);  // a block for every wavefront

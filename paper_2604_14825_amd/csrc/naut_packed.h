@@ -156,6 +156,9 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
             t.Sk = __builtin_amdgcn_readfirstlane(s.Sk);
         }
         t.rows = t.Sq * p.g;
+        // Offsets that fall can give sequences that overlap, more tiles than the sums above hold, and so a tile that is none.
+        if (t.qt < 0 || (long long)t.qt * BM >= t.rows)
+            t.qt = -1;
         return true;
     };
 #pragma unroll

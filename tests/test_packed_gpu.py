@@ -141,6 +141,18 @@ def test_long_sequences(D, Hq, Hkv, lens, causal):
     run(lens, None, Hq, Hkv, D, causal, seed=8)
 
 
+def test_scale_zero_is_the_mean():
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    q, k, v = (torch.randn((90, 2, 64), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
+    o, lse = torch.empty((90, 2, 64), device="cuda"), torch.empty((2, 90), device="cuda")
+    nb.naut_attn_fwd_packed(q, k, v, o, lse, offsets([30, 60]), offsets([30, 60]), True, np.float32(0.0))
+    for first, n in ((0, 30), (30, 60)):
+        want = v[first : first + n].double().cumsum(0).cpu().numpy() / np.arange(1, n + 1)[:, None, None]
+        got = o[first : first + n].double().cpu().numpy()
+        assert np.abs(got - want).max() <= 64 * 2.0 ** -24 * 4  # P is 1 in every place: only the sums round
+        assert np.abs(lse[:, first : first + n].double().cpu().numpy() - np.log(np.arange(1, n + 1))).max() < 1e-5
+
+
 def test_no_rows():
     z = torch.zeros((0, 4, 64), device="cuda", dtype=torch.bfloat16)
     x = torch.full((5, 4, 64), 7.0, device="cuda", dtype=torch.bfloat16)
@@ -158,16 +170,17 @@ def test_offsets_that_make_no_sense_are_empty_sequences():
     gen = torch.Generator(device="cuda").manual_seed(9)
     q, k, v = (torch.randn((300, 2, 64), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
     whole = reference(q[:100], k[:100], v[:100], [100], [100], 0.125, True)
-    for cu_q, cu_k, left in [([0, 100, 90], [0, 100, 200], 100), ([0, 100, 301], [0, 100, 200], 100), ([0, 100, 200], [0, 100, 1 << 30], 100),
+    many = [0, 300] * 500 + [0]  # falling every other time: 500 sequences in the same place, more tiles than a launch has
+    for cu_q, cu_k, left in [(many, many, 300), ([0, 100, 90], [0, 100, 200], 100), ([0, 100, 301], [0, 100, 200], 100), ([0, 100, 200], [0, 100, 1 << 30], 100),
                              ([0, 100, -5], [0, 100, 200], 100), ([0, 100, 200], [0, 100, 50], 100), ([-7, -3], [0, 10], 0),
                              ([0, 100, 0x7fffffff], [0, 100, 0x7fffffff], 100)]:
-        print(cu_q, cu_k, flush=True)
+        print(cu_q[:4], cu_k[:4], flush=True)
         o, lse = torch.full_like(q, 7.0), torch.full((2, 300), 7.0, device="cuda")
         as_t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
         nb.naut_attn_fwd_packed(q, k, v, o, lse, as_t(cu_q), as_t(cu_k), True, 0.125)
         torch.cuda.synchronize()
         assert (o[left:] == 7.0).all() and (lse[:, left:] == 7.0).all()
-        if left:
+        if left == 100:
             su.check(o[:100].double().cpu().numpy(), lse[:, :100].T.double().cpu().numpy(), [whole[0], whole[1], whole[2], whole[3]], "bf16", "bf16", 100, "first sequence")
 
 

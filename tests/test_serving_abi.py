@@ -33,7 +33,8 @@ def but(i, x):
     (dict(scale=float("inf")), nb.NAUT_ERR_SHAPE), (dict(scale=-0.5), nb.NAUT_ERR_UNSUPPORTED), (dict(D=100), nb.NAUT_ERR_UNSUPPORTED),
     (dict(D=264), nb.NAUT_ERR_UNSUPPORTED), (dict(types=(F32, F32)), nb.NAUT_ERR_UNSUPPORTED), (dict(types=(BF, F16)), nb.NAUT_ERR_UNSUPPORTED),
     (dict(Tq=(1 << 30) + 1), nb.NAUT_ERR_UNSUPPORTED), (dict(n=(1 << 20) + 1), nb.NAUT_ERR_UNSUPPORTED),
-    (dict(Tq=1 << 30, Hq=512, Hkv=512), nb.NAUT_ERR_UNSUPPORTED),
+    (dict(Tq=1 << 30, Hq=512, Hkv=512), nb.NAUT_ERR_UNSUPPORTED), (dict(Hq=2048, Hkv=1), nb.NAUT_ERR_UNSUPPORTED), (dict(Hq=1 << 16, Hkv=1 << 16), nb.NAUT_ERR_UNSUPPORTED),
+    (dict(Tk=1 << 29, Hq=8, Hkv=2), nb.NAUT_ERR_UNSUPPORTED),
     (dict(q=A + 8), nb.NAUT_ERR_ALIGN), (dict(v=A + 2), nb.NAUT_ERR_ALIGN), (dict(o=A + 4), nb.NAUT_ERR_ALIGN), (dict(lse=A + 2), nb.NAUT_ERR_ALIGN),
     (dict(cu_q=A + 2), nb.NAUT_ERR_ALIGN), (dict(cu_k=A + 1), nb.NAUT_ERR_ALIGN),
     (dict(st=but(2, 260)), nb.NAUT_ERR_ALIGN), (dict(st=but(5, -128)), nb.NAUT_ERR_ALIGN), (dict(st=but(7, 4)), nb.NAUT_ERR_ALIGN),
@@ -117,7 +118,7 @@ def test_decode_refusals():
         assert decode(c, **kw) == nb.NAUT_ERR_NULL, kw
     for kw in (dict(Hq=0), dict(Hq=3), dict(Sq=0), dict(scale=float("inf")), dict(room=need - 1)):
         assert decode(c, **kw) == nb.NAUT_ERR_SHAPE, kw
-    for kw in (dict(scale=-1.0), dict(types=(F32, F32)), dict(types=(F16, BF)), dict(Sq=1 << 30)):
+    for kw in (dict(scale=-1.0), dict(types=(F32, F32)), dict(types=(F16, BF)), dict(Sq=1 << 30), dict(Hq=1 << 27)):
         assert decode(c, **kw) == nb.NAUT_ERR_UNSUPPORTED, kw
     for kw in (dict(q=A + 8), dict(o=A + 8), dict(ws=A + 8), dict(lse=A + 2), dict(lens=A + 2)):
         assert decode(c, **kw) == nb.NAUT_ERR_ALIGN, kw
