@@ -753,7 +753,6 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         constexpr int RPI = 64 / CPRO;    // rows per store instruction
         constexpr int BATCH = 8 < 32 / RPI ? 8 : 32 / RPI;  // reads in flight before their stores
-        typedef i32x4_t __attribute__((aligned(8))) i32x4_a8;  // O rows are 8-byte aligned, not more
 #pragma unroll
         for (int i0 = 0; i0 < 32 / RPI; i0 += BATCH) {
             i32x4_t rows[BATCH];
@@ -764,7 +763,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
             for (int i = 0; i < BATCH; ++i) {
                 const int q = q_wave0 + (i0 + i) * RPI + ln / CPRO;
                 if (q < Sq && ln % CPRO < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
-                    *(i32x4_a8*)(o_row(q) + (ln % CPRO) * 16) = rows[i];
+                    store_o<PACKED>(o_row(q) + (ln % CPRO) * 16, rows[i]);
             }
         }
     } else if (my_q < Sq) {
@@ -778,7 +777,7 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
                     continue;  // padding columns of a narrower head dimension
                 f32x4_t w = {oacc[db][4 * g + 0] * inv_l, oacc[db][4 * g + 1] * inv_l,
                              oacc[db][4 * g + 2] * inv_l, oacc[db][4 * g + 3] * inv_l};
-                *(f32x4_t*)(og + d * 4) = w;
+                store_o<PACKED>(og + d * 4, w);
             }
     }
 }

@@ -780,7 +780,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
                     *(i32x2_t*)(staged(32 * hf + l32, d >> 3) + (d & 7) * 2) =
                         i32x2_t{In<DT_OUT>::pack2(x.x, x.y), In<DT_OUT>::pack2(x.z, x.w)};
                 else if (q < Sq && d < cpr * 8)  // not the padding columns of a narrower head dimension
-                    *(f32x4_t*)(og + d * 4) = x;
+                    store_o<PACKED>(og + d * 4, x);
             }
     }
     if constexpr (OUTB == 2) {
@@ -788,7 +788,6 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         constexpr int RPI = 64 / CPRO;  // rows per store instruction
-        typedef i32x4_t __attribute__((aligned(8))) i32x4_a8;  // O rows are 8-byte aligned, not more
         i32x4_t rows[WQ / RPI];
 #pragma unroll
         for (int i = 0; i < WQ / RPI; ++i)  // all reads first: one LDS latency, not one per store
@@ -798,7 +797,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
             const int ch = lane % CPRO;
             const int q = Q0 + i * RPI + lane / CPRO;
             if (q < Sq && ch < cpr)  // not the rows beyond Sq, not the padding columns of a narrower head
-                *(i32x4_a8*)(o_row(q) + ch * 16) = rows[i];
+                store_o<PACKED>(o_row(q) + ch * 16, rows[i]);
         }
     }
 }
