@@ -2,11 +2,13 @@
 //
 // The sequences of a batch lie back to back in memory and only the GPU knows their lengths (cu_q and cu_k, offsets of
 // n + 1 entries each), so that the host needs no copy of them and a captured launch follows them.  The grid is an upper
-// bound, and every work-group finds its own tile: a few reductions over the sequences, one to a lane, before its first load.
+// bound, and every work-group finds its own tile before its first load.
 #ifndef NAUT_PACKED_H
 #define NAUT_PACKED_H
 
 namespace naut_k {
+
+constexpr int PACKED_BY_LEVEL = 256;
 
 struct PackedParams : Params {  // batch strides, S and the counts of tiles are not used
     const int* cu_q;
@@ -16,7 +18,8 @@ struct PackedParams : Params {  // batch strides, S and the counts of tiles are 
     int g;        // query heads per K/V head, at most 1024
     unsigned g_inv;  // ceil(2^22 / g)
     int pos_per_tile;  // positions of a tile where they are whole, otherwise 0
-    int class_of[6];   // levels at which a class of tiles ends (see packed_tile), falling
+    int by_level;      // the tiles go by level, not by sequence (see packed_tile; at most PACKED_BY_LEVEL sequences)
+    int class_of[6];   // levels at which a class of tiles ends, falling
 };
 
 template <bool PACKED>
@@ -55,13 +58,46 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b)
     return {q0, k0, ok ? q1 - q0 : 0, ok ? k1 - k0 : 0};
 }
 
-// The work-group's tile, of BM rows.  Heavy tiles come first, as in one long causal sequence: the last tile of a sequence has the
-// level ceil(Sk g / BM) (at least its number of tiles), those before it one less each, and the tiles go by classes of levels,
+// Tile i by sequence, each from its last one.  Sequence b's tiles have the numbers from floor(cu_q[b] g / BM) + b on, which
+// are enough of them without a sum over the sequences before; the sequence of a number is found 64 probes at a time.
+template <int BM>
+__device__ __forceinline__ int packed_number(const PackedParams& p, int b)
+{
+    const int q0 = p.cu_q[b];
+    return (q0 < 0 ? 0 : q0 < p.Tq ? q0 : p.Tq) * p.g / BM + b;
+}
+template <int BM>
+__device__ __forceinline__ void packed_tile_by_sequence(const PackedParams& p, int lane, int i, PackedTile& t)
+{
+    int lo = 0, hi = p.n;  // the sequence is lo or later, and before hi
+    while (hi - lo > 1) {
+        const int step = (hi - lo + 63) >> 6, b = lo + step * (lane + 1);
+        const unsigned long long beyond = __builtin_amdgcn_ballot_w64(b >= hi || packed_number<BM>(p, b) > i);  // (lane 63's b is not before hi)
+        lo += step * __builtin_ctzll(beyond);
+        hi = hi < lo + step ? hi : lo + step;
+    }
+    const PackedSeq s = packed_seq(p, lo);
+    t.q0 = __builtin_amdgcn_readfirstlane(s.q0);
+    t.k0 = __builtin_amdgcn_readfirstlane(s.k0);
+    t.Sq = __builtin_amdgcn_readfirstlane(s.Sq);
+    t.Sk = __builtin_amdgcn_readfirstlane(s.Sk);
+    t.rows = t.Sq * p.g;
+    const int tiles = (t.rows + BM - 1) / BM, at = i - __builtin_amdgcn_readfirstlane(packed_number<BM>(p, lo));
+    t.qt = at >= 0 && at < tiles ? tiles - 1 - at : -1;
+}
+
+// The work-group's tile, of BM rows.  Tiles go by sequence, or, with few sequences, by level: heavy ones come first then, as in one
+// long causal sequence, and none is left to run behind the others, but a work-group looks at every sequence and those of a sequence
+// are apart, which its K and V in the L2s tell.  32/8 heads, D = 128, us by level and by sequence: 8 of 1 to 2048 (D = 64) 71 / 76, 24 of
+// 50 to 1000 (12/12 heads, D = 64) 31.8 / 34.2, 32 of 1 to 512 62 / 57, 128 of 1 to 1000 571 / 547, 512 of 1 to 1000 2633 / 2206, 512 of 1 to
+// 64 129 / 90 (but 64 of 1 to 4 8.4 / 11: more work-groups without a tile); new turns of 1 to 100 behind up to 1500 keys, 64/8 heads, 64 of them 101 / 112, 256 423 / 420.
+//   By level: the last tile of a sequence has the level ceil(Sk g / BM) (at least its number of tiles), those before it one
+// less each, and the tiles go by classes of levels,
 // each half as high as the one before (8, 4, 2, 1, 1/2 and 1/4 of the mean level, which the host knows, and the rest).  Inside
 // a class they go by sequence and fall.  F(L), the tiles at level L or above, is a sum over the sequences, one to a
 // lane; those of all classes are formed at once, so that the steps of one sum hide the latency of another's.  The exact order
-// by levels, found by halving, took every work-group about 1 us longer (64 sequences of 256, 32/8 heads, D = 128, no mask:
-// 142.5 us for 120.0; 14 prompts 172 for 163).  Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
+// by levels, found by halving, took every work-group about 1 us longer (14 prompts 172 us for 163).
+//   Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
 // first axis, an XCD keeps to an eighth of them, whose rows stay in its L2.
 template <int BM>
 __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lane)
@@ -70,8 +106,12 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
     const int x = blockIdx.x, i = (int)(blockIdx.y + blockIdx.z * gridDim.y);
     t.hk = p.Hkv & 7 ? x : (x & 7) * (p.Hkv >> 3) + (x >> 3);
     t.qt = -1;
+    if (!p.by_level) {
+        packed_tile_by_sequence<BM>(p, lane, i, t);
+        return t;
+    }
     const int nch = (p.n + 63) >> 6;  // 64 sequences at a time
-    constexpr int KEPT = 8;           // lots of them that stay in registers; later ones are read again
+    constexpr int KEPT = PACKED_BY_LEVEL / 64;
     constexpr int NC = 7;             // classes
     PackedSeq first = {0, 0, 0, 0};   // of the first 64, for their sequences' own numbers
     int nqt[KEPT], top[KEPT];
@@ -108,11 +148,6 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
             load(c, nqt[c], top[c]);
             add(nqt[c], top[c]);
         }
-    }
-    for (int c = KEPT; c < nch; ++c) {
-        int a, b;
-        load(c, a, b);
-        add(a, b);
     }
     wave_scan(sum);
     int from = 0, lower = 1, upper = 0x7fffffff;  // tiles before the class, its lowest level and that of the class before
@@ -165,12 +200,6 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
     for (int c = 0; c < KEPT; ++c)
         if (c < nch && pick(c, nqt[c], top[c]))
             return t;
-    for (int c = KEPT; c < nch; ++c) {
-        int a, b;
-        load(c, a, b);
-        if (pick(c, a, b))
-            return t;
-    }
     return t;
 }
 

@@ -6,10 +6,15 @@
 
 namespace naut_k {
 
+// Three keys for two queries or more: new turns of conversations that are cached.
+inline bool packed_more_keys(const PackedParams& p) { return 2LL * p.Tk >= 3LL * p.Tq; }
+
 // Tiles of `bm` rows: n sequences of Tq positions in all have at most this many for each K/V head, whatever their lengths.
 inline long long packed_tiles(const PackedParams& p, int bm)
 {
     const long long rows = (long long)p.Tq * p.g, tiles = (rows + (long long)(bm - 1) * p.n) / bm;
+    if (!p.by_level)
+        return rows / bm + p.n;  // the numbers of packed_tile_by_sequence
     return tiles < rows ? tiles : rows;
 }
 
@@ -41,7 +46,7 @@ inline int packed_form(const PackedParams& p, int D, int causal, int* groups)
     if (D > 128)
         return w <= 512 ? V_W4Q32 : V_W8Q32;
     const int keys = p.Tk / p.n;
-    const bool more_keys = 2LL * p.Tk >= 3LL * p.Tq;
+    const bool more_keys = packed_more_keys(p);
     if (more_keys ? w <= (D <= 64 ? 256 : 160) && keys >= 200 : w <= 128 && keys >= 400) {
         *groups = 4;
         return V_BM128;
@@ -63,6 +68,7 @@ int launch_packed(PackedParams p, int causal, hipStream_t stream)
 {
     const int mean = (int)(((long long)(p.Tk > p.Tq ? p.Tk : p.Tq) + p.n - 1) / p.n);
     p.p_limit = long_loops(mean, (long long)p.n * p.Hq, D, causal) ? In<DT_IN>::P_LIMIT : 24.0f;  // as in launch(), for a sequence of mean length
+    p.by_level = p.n > 1 && p.n < (packed_more_keys(p) ? PACKED_BY_LEVEL + 1 : 32);  // both sides' times are at packed_tile
     int groups;
     const int form = packed_form(p, D, causal, &groups);
     if (form == V_W4Q32 && groups == 2 && D <= 128 && (p.k_rs > p.v_rs ? p.k_rs : p.v_rs) > 8 << 20)

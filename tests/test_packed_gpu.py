@@ -117,6 +117,29 @@ def test_many_sequences(n):
     run([int(x) for x in rng.integers(0, 200, n)] if n < 100 else [1] * (n - 2) + [300, 129], None, 2, 1, 128, True, seed=6)
 
 
+@pytest.mark.parametrize("n,first", [(512, 0), (513, 11), (1031, 0), (4097, 5)])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (8, 8, 128), (5, 1, 256)])
+def test_more_sequences_than_are_looked_at(n, first, Hq, Hkv, D):
+    """Where a work-group searches for its sequence: runs of empty ones, one of several tiles at either end and in between."""
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in np.where(rng.random(n) < 0.5, 0, rng.integers(1, 5, n))]
+    lens[n // 2 : n // 2 + 130] = [0] * 130
+    lens[0], lens[n // 3], lens[-1] = 200, 333, 129
+    k_lens = [x + int(y) if x else int(y) for x, y in zip(lens, rng.integers(0, 3, n))]
+    run(lens, k_lens, Hq, Hkv, D, True, first=first, pad=9, seed=13)
+    run([0] * (n - 1) + [70], None, Hq, Hkv, D, False, seed=13)
+
+
+@pytest.mark.parametrize("n", [31, 32, 64, 65, 255, 256, 257])
+@pytest.mark.parametrize("behind", [0, 150])
+def test_orders_of_tiles(n, behind):
+    """By level, one or more lots of 64 sequences in registers, and by sequence."""
+    rng = np.random.default_rng(n)
+    lens = [int(x) for x in rng.integers(0, 90, n)]
+    lens[n // 2] = 400
+    run(lens, [x + int(y) for x, y in zip(lens, rng.integers(0, behind + 1, n))], 4, 2, 64, True, seed=14)
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_maxima_that_move(D):
     run([600, 129], None, 4, 4, D, True, seed=7, magnify=6.0)
