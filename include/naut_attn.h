@@ -314,7 +314,7 @@ int naut_kv4_load(void* k, void* v, const naut_kv4_cache* cache, const int* slot
  * A row that sees nothing has o = 0 and lse = -inf.  Both products run on the cache's values in the type of q (NAUT_F16 as in
  * naut_kv4_load) with fp32 accumulation; the softmax runs in fp32.  The key axis is split by the lengths that the GPU finds,
  * so that a captured call follows them; the partials live in `workspace` (DEVICE memory of the caller, 16-byte aligned, at least
- * naut_attn_decode_kv4_workspace_bytes(...) bytes, overwritten, not shared by calls that may overlap).  One or two kernels.
+ * naut_attn_decode_kv4_workspace_bytes(...) bytes, overwritten, not shared by calls that may overlap).  One to three kernels.
  * `st` gives the batch, head and sequence strides of q and o in elements by the rules of naut_attn_fwd_strided (NULL =
  * contiguous; those of k and v are not looked at).  Types and scale as in naut_attn_decode_dt.
  */

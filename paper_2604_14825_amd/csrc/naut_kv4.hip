@@ -283,6 +283,7 @@ int launched()
 constexpr int KV_SHIFT = 5, KV_BLK = 1 << KV_SHIFT;  // keys per block
 constexpr int KV_FINER = 2;     // how much finer it cuts more sequences than fill the chip
 constexpr int KV_TARGET = 256;  // work-groups that the plan aims at: one to a CU, of eight wavefronts
+constexpr int KV_PLANNED = 256; // sequences from which on a kernel of its own makes the plan (see naut_decode_kv4_plan_kernel)
 constexpr int MRG_WAVES = 4;
 
 struct Kv4Params {
@@ -292,7 +293,7 @@ struct Kv4Params {
     const unsigned char *codes[2], *scales[2];  // K, V
     long long c_b, c_h, c_s, s_b, s_h, s_s;
     const int* lens;
-    float* ws;        // partial O [nparts][rows][D], then m [nparts][rows], l [nparts][rows], then {first split, splits} [B]
+    float* ws;        // partial O [nparts][rows][D], then m [nparts][rows], l [nparts][rows], then {first split, splits} [B] or the plan
     int B, Hq, Hkv, Sq, S;
     int R;            // query rows per (sequence, K/V head)
     int rows;         // of a chunk of them, a multiple of 16
@@ -300,6 +301,8 @@ struct Kv4Params {
     int aim;          // splits of all sequences together that fill the chip
     int P;            // and at most: KV_FINER aim + B, or B where every sequence is one split (the grid)
     int least;        // blocks per split, at least
+    int merges;       // sequences that the merge looks at: B, or, with a plan, those that are split: at most KV_FINER aim
+    int planned;
     int causal;
     float c;          // scale * log2(e), > 0
     int out_f32;
@@ -317,69 +320,102 @@ __device__ __forceinline__ int kv4_len(const Kv4Params& p, int b)
 struct Kv4Split {
     int b, split, nsplit, first;  // sequence, its split, its splits, the index of its first split
     int len, begin, end;          // keys, blocks
+
+    __device__ __forceinline__ void cut(int x)  // from b, nsplit, first and len
+    {
+        const int all = ((len - 1) >> KV_SHIFT) + 1, each = (all + nsplit - 1) / nsplit;
+        split = x - first;
+        begin = split * each < all ? split * each : all;
+        end = begin + each < all ? begin + each : all;
+    }
 };
 
-// Which part of which sequence split x is: every sequence is cut into equal parts of about L blocks (an empty one is one
-// part).  L is the mean, total / aim, where that makes no more than `aim` parts, as it does for lengths that are alike; or up to twice
+// The plan as its kernel leaves it: splits P, then merges, each {sequence or -1, its first split, its splits, its keys}.
+__device__ __forceinline__ i32x4_t* kv4_plan_of(const Kv4Params& p, int D)
+{
+    return (i32x4_t*)(p.ws + (size_t)p.Hkv * p.nchunks * p.P * p.rows * (D + 2));
+}
+
+// Parts of a sequence of n blocks (-1: there is no sequence), rcp = 1 / L.  Need not be the exact quotient: its blocks are dealt out
+// evenly over whatever it is.
+__device__ __forceinline__ int kv4_parts(int n, float rcp)
+{
+    const int m = (int)__builtin_fmaf((float)n, rcp, 0.9999f);
+    return n < 0 ? 0 : m < 1 ? 1 : m;
+}
+
+// How every sequence is cut: into equal parts of about L blocks (an empty one is one part); count(L) gives the parts of all.
+//   L is the mean, total / aim, where that makes no more than `aim` parts, as it does for lengths that are alike; or up to twice
 // the mean if that keeps them to `aim`, found by halving to a sixteenth (a further round of work-groups costs more than longer parts,
 // a longer search more than the shorter parts give); or, with many sequences or one that is most of the batch, half the mean
 // (at most 2 aim + B parts).  32/8 heads, D = 128, us with L = total / max(aim, B) always, the mean, half and a quarter of it: one of
 // 30000 among 47 of 100 keys 115 / 17.5 / 18.1 / 22.1, 100 of 1 to 8192 103 / 108 / 98 / 91, 64 of 5000 60.5 / 64.1 / 63.9 / 68.1.
-// 64 sequences at a time, one to a lane.
+template <typename Count>
+__device__ __forceinline__ int kv4_part_blocks(const Kv4Params& p, int total, Count&& count)
+{
+    int L = (total + p.aim - 1) / p.aim;
+    L = L > p.least ? L : p.least;
+    if (count(L) <= p.aim)
+        return L;
+    if (count(2 * L) <= p.aim) {
+        int lo = L, hi = 2 * L;
+        while (hi - lo > (lo >> 4) + 1) {
+            const int mid = (lo + hi) >> 1;
+            if (count(mid) <= p.aim)
+                hi = mid;
+            else
+                lo = mid;
+        }
+        return hi;
+    }
+    L = (total + p.aim * KV_FINER - 1) / (p.aim * KV_FINER);
+    return L > p.least ? L : p.least;
+}
+
+// Which part of which sequence split x is.  Without a plan every work-group finds it by itself, 64 sequences at a time, one to a lane.
+template <int D>
 __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, Kv4Split* out)
 {
     if (x >= p.P)
         return false;  // the grid is rounded up to eights
     if (p.P == p.B) {  // short caches, or many: a part each
         out->b = x;
-        out->split = out->first = out->begin = 0;
+        out->first = x;
         out->nsplit = 1;
         out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, x));
-        out->end = ((out->len - 1) >> KV_SHIFT) + 1;
+        out->cut(x);
+        return true;
+    }
+    if (p.planned) {
+        const i32x4_t e = kv4_plan_of(p, D)[x];
+        out->b = __builtin_amdgcn_readfirstlane(e.x);
+        out->first = __builtin_amdgcn_readfirstlane(e.y);
+        out->nsplit = __builtin_amdgcn_readfirstlane(e.z);
+        out->len = __builtin_amdgcn_readfirstlane(e.w);
+        if (out->b < 0)
+            return false;
+        out->cut(x);
         return true;
     }
     const int nch = (p.B + 63) >> 6;
     auto blocks = [&](int c) { return c * 64 + lane < p.B ? ((kv4_len(p, c * 64 + lane) - 1) >> KV_SHIFT) + 1 : -1; };
     const int mine = blocks(0);  // the first 64's, kept
     auto of = [&](int c) { return c == 0 ? mine : blocks(c); };
-    // Parts of a sequence of n blocks.  Need not be the exact quotient: its blocks are dealt out evenly over whatever it is.
-    auto parts = [&](int n, float rcp) {
-        const int m = (int)__builtin_fmaf((float)n, rcp, 0.9999f);
-        return n < 0 ? 0 : m < 1 ? 1 : m;
-    };
-    auto count = [&](int L) {
-        const float rcp = __builtin_amdgcn_rcpf((float)L);
-        int sum = parts(mine, rcp);
-        for (int c = 1; c < nch; ++c)
-            sum += parts(blocks(c), rcp);
-        return wave_sum(sum);
-    };
     int total = 0;
     for (int c = 0; c < nch; ++c)
         total += of(c) > 0 ? of(c) : 0;
     total = wave_sum(total);
-    int L = (total + p.aim - 1) / p.aim;
-    L = L > p.least ? L : p.least;
-    if (count(L) > p.aim) {
-        if (count(2 * L) <= p.aim) {
-            int lo = L, hi = 2 * L;
-            while (hi - lo > (lo >> 4) + 1) {
-                const int mid = (lo + hi) >> 1;
-                if (count(mid) <= p.aim)
-                    hi = mid;
-                else
-                    lo = mid;
-            }
-            L = hi;
-        } else {
-            L = (total + p.aim * KV_FINER - 1) / (p.aim * KV_FINER);
-            L = L > p.least ? L : p.least;
-        }
-    }
+    const int L = kv4_part_blocks(p, total, [&](int L) {
+        const float rcp = __builtin_amdgcn_rcpf((float)L);
+        int sum = kv4_parts(mine, rcp);
+        for (int c = 1; c < nch; ++c)
+            sum += kv4_parts(blocks(c), rcp);
+        return wave_sum(sum);
+    });
     const float rcp = __builtin_amdgcn_rcpf((float)L);
     int before = 0;
     for (int c = 0; c < nch; ++c) {
-        const int n = of(c), m = parts(n, rcp);
+        const int m = kv4_parts(of(c), rcp);
         const int incl = wave_scan(m) + before;
         const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > x);
         if (mask == 0) {
@@ -390,15 +426,90 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
         out->b = c * 64 + src;
         out->nsplit = __builtin_amdgcn_readlane(m, src);
         out->first = __builtin_amdgcn_readlane(incl, src) - out->nsplit;
-        out->split = x - out->first;
-        const int all = __builtin_amdgcn_readlane(n, src);
-        const int each = (all + out->nsplit - 1) / out->nsplit;
         out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, out->b));
-        out->begin = out->split * each < all ? out->split * each : all;
-        out->end = out->begin + each < all ? out->begin + each : all;
+        out->cut(x);
         return true;
     }
     return false;
+}
+
+// The plan of many sequences, by one work-group: found by every work-group of the split kernel it takes time that grows with the
+// square of the sequences.  The merge gets the sequences that are split, of which there are at most KV_FINER aim.  32/8 heads,
+// D = 128, lengths of 1 to 2304, us without and with this kernel: 128 sequences 38.9 / 40.0, 256 77 / 69, 1024 406 / 244, 8192 13700 / 1850;
+// 8/1 heads, 1 to 30 keys: 128 12.9 / 15.6, 256 13.1 / 15.2, 512 21.6 / 16.0.
+constexpr int PLAN_THREADS = 1024;
+template <int D>
+__global__ __launch_bounds__(PLAN_THREADS) void naut_decode_kv4_plan_kernel(const Kv4Params p)
+{
+    constexpr int NW = PLAN_THREADS / 64;
+    __shared__ int sums[2][2][NW];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int turn = 0;  // two sets of sums in turn: one barrier each
+    // sums over the wavefronts before this one, and over all
+    auto over_waves = [&](int x, int y, int* x_before, int* y_before, int* x_all, int* y_all) {
+        turn ^= 1;
+        if (lane == 0) {
+            sums[turn][0][wave] = x;
+            sums[turn][1][wave] = y;
+        }
+        __syncthreads();
+        *x_before = *y_before = *x_all = *y_all = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const int a = sums[turn][0][w], b = sums[turn][1][w];
+            *x_before += w < wave ? a : 0;
+            *y_before += w < wave ? b : 0;
+            *x_all += a;
+            *y_all += b;
+        }
+    };
+    auto len_of = [&](int b) { return b < p.B ? kv4_len(p, b) : -KV_BLK; };
+    auto blocks = [&](int len) { return ((len - 1) >> KV_SHIFT) + 1; };  // (no sequence: -1)
+    static_assert(((-KV_BLK - 1) >> KV_SHIFT) + 1 == -1);
+    auto all_of = [&](int x) {
+        int a, b, c, d;
+        over_waves(wave_sum(x), 0, &a, &b, &c, &d);
+        return __builtin_amdgcn_readfirstlane(c);
+    };
+    int total = 0;
+    for (int b = tid; b < p.B; b += PLAN_THREADS)
+        total += blocks(len_of(b));
+    total = all_of(total);
+    const int L = kv4_part_blocks(p, total, [&](int L) {
+        const float rcp = __builtin_amdgcn_rcpf((float)L);
+        int sum = 0;
+        for (int b = tid; b < p.B; b += PLAN_THREADS)
+            sum += kv4_parts(blocks(len_of(b)), rcp);
+        return all_of(sum);
+    });
+    const float rcp = __builtin_amdgcn_rcpf((float)L);
+    i32x4_t* const plan = kv4_plan_of(p, D);
+    int parts = 0, merges = 0;  // of the sequences so far
+    for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
+        const int b = b0 + tid, len = len_of(b), m = kv4_parts(blocks(len), rcp), s = m > 1;
+        const int m_incl = wave_scan(m), s_incl = wave_scan(s);
+        int mb, sb, ma, sa;
+        over_waves(__builtin_amdgcn_readlane(m_incl, 63), __builtin_amdgcn_readlane(s_incl, 63), &mb, &sb, &ma, &sa);
+        const int first = parts + mb + m_incl - m, at = merges + sb + s_incl - s;
+        if (m > 0 && first < p.P)
+            plan[first] = i32x4_t{b, first, m, len};
+        if (s && at < p.merges)
+            plan[p.P + at] = i32x4_t{b, first, m, len};
+        // the other parts of a sequence, by the wavefront
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(s); left != 0; left &= left - 1) {
+            const int src = __builtin_ctzll(left);
+            const i32x4_t e = {b0 + wave * 64 + src, __builtin_amdgcn_readlane(first, src), __builtin_amdgcn_readlane(m, src), __builtin_amdgcn_readlane(len, src)};
+            for (int i = 1 + lane; i < e.z; i += 64)
+                if (e.y + i < p.P)
+                    plan[e.y + i] = e;
+        }
+        parts += __builtin_amdgcn_readfirstlane(ma);
+        merges += __builtin_amdgcn_readfirstlane(sa);
+    }
+    for (int x = parts + tid; x < p.P; x += PLAN_THREADS)
+        plan[x] = i32x4_t{-1, 0, 0, 0};
+    for (int x = merges + tid; x < p.merges; x += PLAN_THREADS)
+        plan[p.P + x] = i32x4_t{-1, 0, 0, 0};
 }
 
 // A row of O (four values at d) and, from one thread, of lse: row r of (sequence b, K/V head hk).
@@ -471,7 +582,7 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     const int eight = p.aim & 7 ? 0 : 3, y = blockIdx.x >> eight, x_of = (blockIdx.y << eight) + (blockIdx.x & ((1 << eight) - 1));
     const int chunk = p.nchunks == 1 ? 0 : y / p.Hkv, hk = y - chunk * p.Hkv;
     Kv4Split sp;
-    if (!kv4_split(p, x_of, lane, &sp))
+    if (!kv4_split<D>(p, x_of, lane, &sp))
         return;
     const int b = sp.b, len = sp.len;
     const int g = p.Hq / p.Hkv;
@@ -687,7 +798,7 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
     float* const ws_m = p.ws + nparts * p.rows * D;
     float* const ws_l = ws_m + nparts * p.rows;
-    if (sp.split == 0 && chunk == 0 && hk == 0 && tid == 0 && p.P > p.B) {  // for the merge
+    if (sp.split == 0 && chunk == 0 && hk == 0 && tid == 0 && p.P > p.B && !p.planned) {  // for the merge
         int* const at = (int*)(ws_l + nparts * p.rows) + 2 * b;
         at[0] = sp.first;
         at[1] = sp.nsplit;
@@ -729,15 +840,24 @@ __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(c
     __shared__ float red_m[MRG_WAVES], red_l[MRG_WAVES];
     __shared__ __attribute__((aligned(16))) float red_o[MRG_WAVES][D];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+    const int row = blockIdx.x, hk = blockIdx.y;
     const int chunk = row / p.rows, r = row % p.rows;
     const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
     const float* ws_m = p.ws + nparts * p.rows * D;
     const float* ws_l = ws_m + nparts * p.rows;
-    const int* const at = (const int*)(ws_l + nparts * p.rows) + 2 * b;
-    const int first = at[0], nsplit = at[1];
+    int b = blockIdx.z, first, nsplit;
+    if (p.planned) {
+        const i32x4_t e = kv4_plan_of(p, D)[p.P + b];
+        b = e.x;
+        first = e.y;
+        nsplit = e.z;
+    } else {
+        const int* const at = (const int*)(ws_l + nparts * p.rows) + 2 * b;
+        first = at[0];
+        nsplit = at[1];
+    }
     if (nsplit <= 1)
-        return;  // stored already
+        return;  // stored already, or no sequence
     const size_t part0 = (size_t)(hk * p.nchunks + chunk) * p.P + first;
     ws_m += part0 * p.rows + r;
     ws_l += part0 * p.rows + r;
@@ -826,13 +946,22 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
     p->aim = (int)aim;
     p->P = (int)P;
     p->least = (int)least;
-    *bytes = P > B ? ((size_t)Hkv * nchunks * P * rows * (kv4_width(D) + 2) * sizeof(float) + (size_t)B * 2 * sizeof(int) + 15) / 16 * 16 : 16;
+    p->planned = P > B && B >= KV_PLANNED;
+    p->merges = p->planned && B > KV_FINER * aim ? (int)aim * KV_FINER : B;
+    const size_t ints = p->planned ? ((size_t)P + p->merges) * 4 : (size_t)B * 2;
+    *bytes = P > B ? ((size_t)Hkv * nchunks * P * rows * (kv4_width(D) + 2) * sizeof(float) + ints * sizeof(int) + 15) / 16 * 16 : 16;
     return true;
 }
 
 template <int D, int DT>
 int launch_kv4(const Kv4Params& p, hipStream_t stream)
 {
+    if (p.planned) {
+        hipLaunchKernelGGL((naut_decode_kv4_plan_kernel<D>), dim3(1), dim3(PLAN_THREADS), 0, stream, p);
+        const int rc = launched();
+        if (rc != NAUT_OK)
+            return rc;
+    }
     const unsigned eight = p.aim & 7 ? 1 : 8;
     const dim3 grid((unsigned)(p.Hkv * p.nchunks) * eight, ((unsigned)p.P + eight - 1) / eight);
     if (p.rows == 16)
@@ -842,7 +971,7 @@ int launch_kv4(const Kv4Params& p, hipStream_t stream)
     const int rc = launched();
     if (rc != NAUT_OK || p.P <= p.B)  // one split each
         return rc;
-    hipLaunchKernelGGL((naut_decode_kv4_merge_kernel<D, DT>), dim3((unsigned)p.R, (unsigned)p.Hkv, (unsigned)p.B), dim3(MRG_WAVES * 64), 0, stream, p);
+    hipLaunchKernelGGL((naut_decode_kv4_merge_kernel<D, DT>), dim3((unsigned)p.R, (unsigned)p.Hkv, (unsigned)p.merges), dim3(MRG_WAVES * 64), 0, stream, p);
     return launched();
 }
 

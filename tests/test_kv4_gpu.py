@@ -205,6 +205,49 @@ def test_more_sequences_than_fill_the_chip():
     run(4, 4, 1, 2500, 128, [2500] * 70, seed=14)
 
 
+@pytest.mark.parametrize("B", [255, 256, 257, 1025])
+def test_many_unlike_sequences(B):
+    """The plan of many: empty ones, one that is cut into many parts, few or none that are cut."""
+    rng = np.random.default_rng(B)
+    lens = [int(x) for x in np.where(rng.random(B) < 0.5, 0, rng.integers(1, 100, B))]
+    H = 1 if B > 1000 else 3
+    run(H, H, 1, 2080, 32, lens, seed=15)
+    lens[0], lens[B // 2], lens[-1] = 2080, 2000, 2079
+    run(2 * H, H, 1, 2080, 64, lens, seed=15)
+    run(3, 1, 2, 4200, 32, lens, False, "f16", "f32", seed=15)
+    run(2, 1, 1, 2080, 32, [0] * B, seed=15)
+
+
+def test_a_plan_in_a_captured_call_follows_the_lengths():
+    B, S = 300, 2200
+    cache = filled(B, 2, S, 64, [S] * B, "bf16")
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    q = torch.randn((B, 4, 1, 64), device="cuda", generator=gen).to(torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty((B, 4, 1), device="cuda")
+    ws = torch.empty(nb.decode_kv4_workspace_bytes(B, 4, 2, 1, S, 64), dtype=torch.uint8, device="cuda")
+    lens = slots_of([S] * B)
+    call = lambda: nb.naut_attn_decode_kv4(q, o, lse, cache, lens, True, 0.125, ws)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    rng = np.random.default_rng(16)
+    for these in ([7] * B, [0] * (B - 1) + [S], [int(x) for x in rng.integers(0, S + 1, B)], [S] * B):
+        lens.copy_(slots_of(these))
+        ws.fill_(0xFF)
+        o.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = o.clone(), lse.clone()
+        ws.zero_()
+        o.fill_(7.0)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(got, o) and torch.equal(got_lse, lse)
+        su.check(o.double().cpu().numpy(), lse.double().cpu().numpy(), reference(q, cache, these, 0.125, True), "bf16", "bf16", S, "replayed plan")
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_maxima_that_move(D):
     run(8, 2, 2, 900, D, [900, 411], seed=7, magnify=8.0)
