@@ -122,10 +122,11 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     // groups cost nothing).
     int qt, hq, Sq, Sk;  // (PACKED: hq is the first of the K/V head's, Sq counts rows)
     long long q_first, k_first, v_first, o_first, lse_first;  // bytes (lse: values) to the sequence's first row
-    int ahead = 0;                   // keys before the first query's own
+    int ahead = 0;                   // PACKED: keys before the first query's own
     int pos0 = 0, head0 = 0;         // PACKED: position and head of the tile's first row
     int pos_end = 0;                 // and the position behind its last row's
     if constexpr (PACKED) {
+        static_assert(CAUSAL, "no mask is one that leaves every key: p.all_keys");
         const PackedTile t = packed_tile<BM>(p, lane);
         if (t.qt < 0)
             return;
@@ -133,11 +134,11 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         hq = t.hk * p.g;
         Sq = t.rows;
         Sk = t.Sk;
-        ahead = Sk - t.Sq;
+        ahead = p.all_keys ? Sk - 1 : Sk - t.Sq;
         pos0 = p.pos_per_tile ? qt * p.pos_per_tile : qt * BM / p.g;
         head0 = qt * BM - pos0 * p.g;
         pos_end = packed_row(p, pos0, head0, (Sq - qt * BM < BM ? Sq - qt * BM : BM) - 1).pos + 1;
-        if (Sk == 0 || (CAUSAL && pos_end + ahead <= 0)) {
+        if (Sk == 0 || pos_end + ahead <= 0) {
             packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, t, qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
             return;
         }
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
         }
     }
     int kv_end_wg = Sk, kv_end_w = Q0 >= Sq ? 0 : Sk;
-    if constexpr (CAUSAL && PACKED) {
+    if constexpr (PACKED) {
         const int w = packed_row(p, pos0, head0, (Sq - Q0 < WQ ? Sq - Q0 : WQ) - 1 + wave * WQ).pos + 1 + ahead;
         kv_end_wg = Sk < pos_end + ahead ? Sk : pos_end + ahead;
         kv_end_w = Q0 >= Sq || w < 0 ? 0 : w < Sk ? w : Sk;
