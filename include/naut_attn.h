@@ -258,7 +258,7 @@ size_t naut_attn_decode_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * sequences or more, cu_q falling at one may leave others out, too: their rows of o and lse stay as they are).
  * `st` gives the head and sequence (row) strides in elements, by the rules of naut_attn_fwd_strided; the batch strides are not
  * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Hq/Hkv at most 1024, Tq and Tk times that
- * at most 2^30, Hkv at most 65535, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
+ * at most 2^30 - 1024, Hkv at most 65535, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.
  */
 int naut_attn_fwd_packed(const void* q, const void* k, const void* v, void* o, float* lse, const int* cu_q,
                          const int* cu_k, int n, int Tq, int Tk, int Hq, int Hkv, int D, int causal, float scale,

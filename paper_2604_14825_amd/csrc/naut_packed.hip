@@ -42,8 +42,9 @@ extern "C" int naut_attn_fwd_packed(const void* q, const void* k, const void* v,
     if ((in_dtype != NAUT_BF16 && in_dtype != NAUT_F16) || (out_dtype != in_dtype && out_dtype != NAUT_F32))
         return fail(NAUT_ERR_UNSUPPORTED, "supported dtypes: q/k/v bf16 or f16; o of the same type or f32");
     const int g = Hq / Hkv;
-    if (g > 1024 || Hkv > 65535 || (long long)Tq * g > 1 << 30 || (long long)Tk * g > 1 << 30 || n > 1 << 20)
-        return fail(NAUT_ERR_UNSUPPORTED, "at most 2^20 sequences, 65535 K/V heads, Hq/Hkv 1024, Tq and Tk times Hq/Hkv 2^30");
+    constexpr long long most = (1 << 30) - 1024;  // a position of a tile plus the keys before it fits 32 bits, those behind the last one too
+    if (g > 1024 || Hkv > 65535 || (long long)Tq * g > most || (long long)Tk * g > most || n > 1 << 20)
+        return fail(NAUT_ERR_UNSUPPORTED, "at most 2^20 sequences, 65535 K/V heads, Hq/Hkv 1024, Tq and Tk times Hq/Hkv 2^30 - 1024");
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15u)
         return fail(NAUT_ERR_ALIGN, "q, k, v and o must be 16-byte aligned");
     if (((uintptr_t)lse | (uintptr_t)cu_q | (uintptr_t)cu_k) & 3u)

@@ -33,6 +33,7 @@ def but(i, x):
     (dict(scale=float("inf")), nb.NAUT_ERR_SHAPE), (dict(scale=-0.5), nb.NAUT_ERR_UNSUPPORTED), (dict(D=100), nb.NAUT_ERR_UNSUPPORTED),
     (dict(D=264), nb.NAUT_ERR_UNSUPPORTED), (dict(types=(F32, F32)), nb.NAUT_ERR_UNSUPPORTED), (dict(types=(BF, F16)), nb.NAUT_ERR_UNSUPPORTED),
     (dict(Tq=(1 << 30) + 1), nb.NAUT_ERR_UNSUPPORTED), (dict(n=(1 << 20) + 1), nb.NAUT_ERR_UNSUPPORTED),
+    (dict(Tk=(1 << 30) - 1023, Hq=1, Hkv=1), nb.NAUT_ERR_UNSUPPORTED), (dict(Tq=(1 << 29) - 511), nb.NAUT_ERR_UNSUPPORTED),
     (dict(Tq=1 << 30, Hq=512, Hkv=512), nb.NAUT_ERR_UNSUPPORTED), (dict(Hq=2048, Hkv=1), nb.NAUT_ERR_UNSUPPORTED), (dict(Hq=1 << 16, Hkv=1 << 16), nb.NAUT_ERR_UNSUPPORTED),
     (dict(Tk=1 << 29, Hq=8, Hkv=2), nb.NAUT_ERR_UNSUPPORTED),
     (dict(q=A + 8), nb.NAUT_ERR_ALIGN), (dict(v=A + 2), nb.NAUT_ERR_ALIGN), (dict(o=A + 4), nb.NAUT_ERR_ALIGN), (dict(lse=A + 2), nb.NAUT_ERR_ALIGN),
