@@ -9,6 +9,7 @@
 namespace naut_k {
 
 constexpr int PACKED_BY_LEVEL = 256;
+constexpr int PACKED_COUNTED = 128;
 
 struct PackedParams : Params {  // batch strides, S and the counts of tiles are not used
     const int* cu_q;
@@ -59,7 +60,44 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b)
     return {q0, k0, ok ? q1 - q0 : 0, ok ? k1 - k0 : 0};
 }
 
-// Tile i by sequence, each from its last one.  Sequence b's tiles have the numbers from floor(cu_q[b] g / BM) + b on, which
+// Tile i by sequence, each from its last one.  Up to PACKED_COUNTED sequences: by their tiles' sums, so that the numbers that no
+// tile has come last.  Between others they would take places on the chip that a tile of its last round needs (32/8 heads, D = 128, 64
+// sequences of 1 to 4, as many work-groups with a tile as fit at once: 7.3 us, numbered as below 10.9; 128 of 1 to 16 14.4 / 17.7, of
+// 1 to 200 61.9 / 63.7; 12 to 256 rows with the sums of 256 sequences up to 1.1 times as long).
+template <int BM>
+__device__ __forceinline__ void packed_tile_by_count(const PackedParams& p, int lane, int i, PackedTile& t)
+{
+    constexpr int KEPT = PACKED_COUNTED / 64;
+    PackedSeq s[KEPT];
+#pragma unroll
+    for (int c = 0; c < KEPT; ++c) {
+        s[c] = {0, 0, 0, 0};
+        if (c * 64 + lane < p.n)
+            s[c] = packed_seq(p, c * 64 + lane);
+    }
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < KEPT; ++c)
+        if (c * 64 < p.n) {
+            const int incl = before + wave_scan((s[c].Sq * p.g + BM - 1) / BM);
+            const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > i);
+            if (mask != 0) {
+                const int src = __builtin_ctzll(mask);
+                t.q0 = __builtin_amdgcn_readlane(s[c].q0, src);
+                t.k0 = __builtin_amdgcn_readlane(s[c].k0, src);
+                t.Sq = __builtin_amdgcn_readlane(s[c].Sq, src);
+                t.Sk = __builtin_amdgcn_readlane(s[c].Sk, src);
+                t.rows = t.Sq * p.g;
+                t.qt = __builtin_amdgcn_readlane(incl, src) - 1 - i;
+                if (t.qt < 0 || (long long)t.qt * BM >= t.rows)
+                    t.qt = -1;  // offsets that fall: sequences that overlap, and a sum that need not fit 32 bits
+                return;
+            }
+            before = __builtin_amdgcn_readlane(incl, 63);
+        }
+}
+
+// More sequences: sequence b's tiles have the numbers from floor(cu_q[b] g / BM) + b on, which
 // are enough of them without a sum over the sequences before; the sequence of a number is found 64 probes at a time.
 template <int BM>
 __device__ __forceinline__ int packed_number(const PackedParams& p, int b)
@@ -89,9 +127,9 @@ __device__ __forceinline__ void packed_tile_by_sequence(const PackedParams& p, i
 
 // The work-group's tile, of BM rows.  Tiles go by sequence, or, with few sequences, by level: heavy ones come first then, as in one
 // long causal sequence, and none is left to run behind the others, but a work-group looks at every sequence and those of a sequence
-// are apart, which its K and V in the L2s tell.  32/8 heads, D = 128, us by level and by sequence: 8 of 1 to 2048 (D = 64) 71 / 76, 24 of
-// 50 to 1000 (12/12 heads, D = 64) 31.8 / 34.2, 32 of 1 to 512 62 / 57, 128 of 1 to 1000 571 / 547, 512 of 1 to 1000 2633 / 2206, 512 of 1 to
-// 64 129 / 90 (but 64 of 1 to 4 8.4 / 11: more work-groups without a tile); new turns of 1 to 100 behind up to 1500 keys, 64/8 heads, 64 of them 101 / 112, 256 423 / 420.
+// are apart, which its K and V in the L2s tell.  32/8 heads, D = 128, us by level and by sequence: 16 of 1 to 2000 152 / 157, 24 of
+// 50 to 1000 (12/12 heads, D = 64) 33.3 / 36.2, 32 of 1 to 512 47.7 / 45.7, 128 of 1 to 1000 583 / 556, 256 of 1 to 64 55.7 / 49.7, 64 of 1
+// to 4 7.9 / 7.4; new turns of 1 to 100 behind up to 1500 keys, 64/8 heads, 64 of them 100 / 109, 100 190 / 196, 256 430 / 434.
 //   By level: the last tile of a sequence has the level ceil(Sk g / BM) (at least its number of tiles), those before it one
 // less each, and the tiles go by classes of levels,
 // each half as high as the one before (8, 4, 2, 1, 1/2 and 1/4 of the mean level, which the host knows, and the rest).  Inside
@@ -108,7 +146,10 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
     t.hk = p.Hkv & 7 ? x : (x & 7) * (p.Hkv >> 3) + (x >> 3);
     t.qt = -1;
     if (!p.by_level) {
-        packed_tile_by_sequence<BM>(p, lane, i, t);
+        if (p.n <= PACKED_COUNTED)
+            packed_tile_by_count<BM>(p, lane, i, t);
+        else
+            packed_tile_by_sequence<BM>(p, lane, i, t);
         return t;
     }
     const int nch = (p.n + 63) >> 6;  // 64 sequences at a time

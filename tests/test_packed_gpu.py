@@ -140,6 +140,20 @@ def test_orders_of_tiles(n, behind):
     run(lens, [x + int(y) for x, y in zip(lens, rng.integers(0, behind + 1, n))], 4, 2, 64, True, seed=14)
 
 
+@pytest.mark.parametrize("n", [33, 64, 65, 127, 128, 129, 130])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (16, 8, 128), (5, 1, 256)])
+def test_counted_sequences(n, Hq, Hkv, D):
+    """Up to 128 sequences their tiles are counted, beyond that numbered: empty ones, one row each, several tiles at either end and
+    where a lane's lot of 64 changes, fewer keys than queries."""
+    rng = np.random.default_rng(n)
+    run([1] * n, None, Hq, Hkv, D, True, seed=16)
+    run([0] * (n - 1) + [140], None, Hq, Hkv, D, False, seed=16)
+    lens = [int(x) for x in rng.integers(0, 6, n)]
+    for i in (0, 31, 32, 62, 63, 64, n - 1):
+        lens[min(i, n - 1)] = int(rng.integers(60, 290))
+    run(lens, [int(x) for x in np.maximum(0, np.array(lens) + rng.integers(-2, 3, n))], Hq, Hkv, D, True, first=7, pad=5, seed=16)
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_maxima_that_move(D):
     run([600, 129], None, 4, 4, D, True, seed=7, magnify=6.0)
