@@ -61,9 +61,9 @@ __device__ __forceinline__ PackedSeq packed_seq(const PackedParams& p, int b)
 }
 
 // Tile i by sequence, each from its last one.  Up to PACKED_COUNTED sequences: by their tiles' sums, so that the numbers that no
-// tile has come last.  Between others they would take places on the chip that a tile of its last round needs (32/8 heads, D = 128, 64
-// sequences of 1 to 4, as many work-groups with a tile as fit at once: 7.3 us, numbered as below 10.9; 128 of 1 to 16 14.4 / 17.7, of
-// 1 to 200 61.9 / 63.7; 12 to 256 rows with the sums of 256 sequences up to 1.1 times as long).
+// tile has come last.  Between others they would take places on the chip that a tile of its last round needs (32/8 heads, D = 128,
+// 64 sequences of 1 to 4, as many work-groups with a tile as fit at once: 7.4 us, numbered as below 10.7; 128 of 1 to 16 14.4 / 17.7, of
+// 1 to 200 61.9 / 63.7).  The sums of 256 sequences cost as much as they give (256 of 1 to 200 139 for 136, of 1 to 16 27.5 for 28.8).
 template <int BM>
 __device__ __forceinline__ void packed_tile_by_count(const PackedParams& p, int lane, int i, PackedTile& t)
 {
