@@ -131,11 +131,12 @@ __device__ __forceinline__ void packed_tile_by_sequence(const PackedParams& p, i
 // 50 to 1000 (12/12 heads, D = 64) 33.3 / 36.2, 32 of 1 to 512 47.7 / 45.7, 128 of 1 to 1000 583 / 556, 256 of 1 to 64 55.7 / 49.7, 64 of 1
 // to 4 7.9 / 7.4; new turns of 1 to 100 behind up to 1500 keys, 64/8 heads, 64 of them 100 / 109, 100 190 / 196, 256 430 / 434.
 //   By level: the last tile of a sequence has the level ceil(Sk g / BM) (at least its number of tiles), those before it one
-// less each, and the tiles go by classes of levels,
-// each half as high as the one before (8, 4, 2, 1, 1/2 and 1/4 of the mean level, which the host knows, and the rest).  Inside
-// a class they go by sequence and fall.  F(L), the tiles at level L or above, is a sum over the sequences, one to a
-// lane; those of all classes are formed at once, so that the steps of one sum hide the latency of another's.  The exact order
-// by levels, found by halving, took every work-group about 1 us longer (14 prompts 172 us for 163).
+// less each, as their loops end sooner.  Without the mask a sequence's loops are alike, and all of its tiles have its level (as with the
+// mask they would leave the first tiles of long sequences to run behind the others: 6 of 1 to 1646 78.8 us for 88.9, 14 of 1 to 4785,
+// 16/16 heads, D = 64 128 for 154).  The tiles go by classes of levels, each half as high as the one before (8, 4, 2, 1, 1/2 and 1/4 of
+// the mean level, which the host knows, and the rest).  Inside a class they go by sequence and fall.  F(L), the tiles at level L or
+// above, is a sum over the sequences, one to a lane; those of all classes are formed at once, so that the steps of one sum hide the
+// latency of another's.  The exact order by levels, found by halving, took every work-group about 1 us longer (14 prompts 172 us for 163).
 //   Work-groups are dealt to the XCDs by linear id mod 8: where eight divides the K/V heads, which are the grid's
 // first axis, an XCD keeps to an eighth of them, whose rows stay in its L2.
 template <int BM>
@@ -157,21 +158,23 @@ __device__ __forceinline__ PackedTile packed_tile(const PackedParams& p, int lan
     constexpr int NC = 7;             // classes
     PackedSeq first = {0, 0, 0, 0};   // of the first 64, for their sequences' own numbers
     int nqt[KEPT], top[KEPT];
+    const bool alike = p.all_keys != 0;  // the tiles of a sequence
     auto load = [&](int c, int& tiles, int& level) {
         tiles = level = 0;
         if (c * 64 + lane < p.n) {
             const PackedSeq s = packed_seq(p, c * 64 + lane);
             tiles = (s.Sq * p.g + BM - 1) / BM;
             const int keys = (s.Sk * p.g + BM - 1) / BM;
-            level = tiles > keys ? tiles : keys;
+            const int least = alike ? 1 : tiles;
+            level = least > keys ? least : keys;
             if (c == 0)
                 first = s;
         }
     };
     // a sequence's tiles at level L or above
     auto part = [&](int tiles, int level, int L) {
-        const int y = level - L + 1;
-        return y < 0 ? 0 : y < tiles ? y : tiles;
+        const int y = level - L + 1, m = alike ? tiles : y;
+        return y <= 0 ? 0 : m < tiles ? m : tiles;
     };
     int sum[NC];
 #pragma unroll

@@ -154,6 +154,20 @@ def test_counted_sequences(n, Hq, Hkv, D):
     run(lens, [int(x) for x in np.maximum(0, np.array(lens) + rng.integers(-2, 3, n))], Hq, Hkv, D, True, first=7, pad=5, seed=16)
 
 
+@pytest.mark.parametrize("n", [2, 3, 30, 31, 64, 65, 256])
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 64), (16, 8, 128), (3, 3, 256)])
+def test_orders_of_tiles_without_a_mask(n, Hq, Hkv, D):
+    """By level all tiles of a sequence go together: of unlike lengths, with keys only, queries only, fewer keys than queries."""
+    rng = np.random.default_rng(n)
+    top = 900 if n < 10 else 300 if n < 40 else 40
+    lens = [int(x) for x in rng.integers(1, top, n)]
+    keys = [int(x) for x in rng.integers(0, top, n) + np.where(rng.random(n) < 0.3, 2 * top, 0)]
+    lens[-1], keys[0] = 3 * top, 0
+    run(lens, lens, Hq, Hkv, D, False, seed=17)
+    run(lens, keys, Hq, Hkv, D, False, first=3, pad=2, seed=17)
+    run([0] + lens[1:], [5] + [x + 2 * top for x in lens[1:]], Hq, Hkv, D, False, seed=17)   # the rule of more keys than queries
+
+
 @pytest.mark.parametrize("D", [64, 128, 256])
 def test_maxima_that_move(D):
     run([600, 129], None, 4, 4, D, True, seed=7, magnify=6.0)
