@@ -254,8 +254,9 @@ size_t naut_attn_decode_workspace_bytes(int B, int Hq, int Hkv, int Sq, int Sk, 
  * 0 .. Sk-Sq+i: its queries are its last Sq positions, and Sq == Sk is the mask of naut_attn_fwd.  A row that sees nothing
  * (no keys, or with `causal` fewer keys than queries) has o = 0 and lse = -inf.  Lengths of 0 and 1 are ordinary.  Rows of o
  * and lse that belong to no sequence are left as they are, and rows of k and v outside a sequence do not reach its results,
- * whatever they hold.  A pair of offsets that falls, is negative or passes Tq or Tk makes its sequence empty (of 32
- * sequences or more, cu_q falling at one may leave others out, too: their rows of o and lse stay as they are).
+ * whatever they hold.  Offsets that are no such offsets do no harm outside o and lse: a pair that falls, is negative or passes
+ * Tq or Tk makes its sequence empty, and where cu_q falls at any pair, other sequences may be left out, too, in whole or in part
+ * (the grid is sized for sequences that share no rows): what is left out of o and lse stays as it is.
  * `st` gives the head and sequence (row) strides in elements, by the rules of naut_attn_fwd_strided; the batch strides are not
  * looked at, NULL means contiguous.  D, the types and scale as in naut_attn_fwd_strided.  Hq/Hkv at most 1024, Tq and Tk times that
  * at most 2^30 - 1024, Hkv at most 65535, n at most 2^20; n or Tq may be 0 (nothing is done).  One kernel, no workspace.

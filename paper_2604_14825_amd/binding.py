@@ -544,7 +544,8 @@ def naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, causal: bool, scale: float
     """Attention forward on packed sequences of different lengths.
 
     q,o [Tq,Hq,D]; k,v [Tk,Hkv,D] (the last axis contiguous, head and row strides of whole 16 bytes); lse contiguous fp32 [Hq,Tq] or
-    None; cu_q, cu_k contiguous int32 device tensors [n+1], the offsets of the n sequences' rows (they may be one tensor).
+    None; cu_q, cu_k contiguous int32 device tensors [n+1], the offsets of the n sequences' rows (they may be one tensor), which
+    must not fall: where cu_q does, rows of any sequence may be left as they are.
     The queries of a sequence are the last positions of its keys.  Rows of no sequence are left as they are, a row that
     sees no key gets o = 0 and lse = -inf.  Enqueues on `stream` and returns; the lengths are read on the GPU."""
     import torch

@@ -235,6 +235,30 @@ def test_offsets_that_make_no_sense_are_empty_sequences():
             su.check(o[:100].double().cpu().numpy(), lse[:, :100].T.double().cpu().numpy(), [whole[0], whole[1], whole[2], whole[3]], "bf16", "bf16", 100, "first sequence")
 
 
+@pytest.mark.parametrize("variant", ["", "w4q32", "w8q32", "bm128g4"])
+@pytest.mark.parametrize("turns,length,causal", [(1, 3000, True), (15, 400, True), (15, 400, False), (30, 130, True), (60, 300, False), (500, 300, True)])
+def test_sequences_that_share_rows_are_right_or_left_out(turns, length, causal, variant, monkeypatch):
+    """Offsets that rise and fall in turn give sequences in the same place, with more tiles than the grid has, whichever order
+    the tiles go in: every row of them is the sequence's result or was not touched, and no other row is written."""
+    monkeypatch.setenv("NAUT_ATTN_VARIANT", variant)
+    print("shared rows", turns, length, causal, variant, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(18)
+    guard = 37
+    q, k, v = (torch.randn((length + guard, 2, 64), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
+    ref = reference(q[:length], k[:length], v[:length], [length], [length], 0.125, causal)
+    cu = torch.tensor([0, length] * (turns + 1), dtype=torch.int32, device="cuda")
+    o, lse = torch.full_like(q, 7.0), torch.full((2, length + guard), 7.0, device="cuda")
+    nb.naut_attn_fwd_packed(q, k, v, o, lse, cu, cu, causal, 0.125)
+    torch.cuda.synchronize()
+    on, ln = o.double().cpu().numpy(), lse.T.double().cpu().numpy()
+    assert (on[length:] == 7.0).all() and (ln[length:] == 7.0).all()
+    left = (on[:length] == 7.0).all(2)
+    assert ((ln[:length] == 7.0) == left).all()
+    on, ln = np.where(left[..., None], ref[0], on[:length]), np.where(left, ref[1], ln[:length])
+    su.check(on, ln, ref, "bf16", "bf16", length, "shared rows")
+    assert not left.all()
+
+
 def test_calls_repeat_bit_for_bit_and_on_another_stream():
     a, la = run([333, 1, 90], None, 8, 2, 128, True, seed=10)
     s = torch.cuda.Stream()
