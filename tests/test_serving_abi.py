@@ -137,6 +137,13 @@ def test_sizes():
     assert w(1, 8, 2, 1, 100, 128) > 0 and w(1, 32, 8, 1, 1 << 20, 128) < 64 << 20   # the partials do not grow with the cache
 
 
+def test_workspace_where_the_positions_pass_32_bits():
+    w = nb.decode_kv4_workspace_bytes
+    assert w(1, 8, 2, 1, (1 << 31) - 1, 128) > 0 and w(2, 8, 2, 1, 1 << 30, 128) == 0 and w(65023, 8, 2, 1, 33025, 128) > 0
+    assert w(65023, 8, 2, 1, 33027, 128) == 0    # 2^31 + 30973 positions
+    assert w(65024, 8, 2, 1, 64, 128) == 0       # more sequences than a grid has with the parts of the split ones
+
+
 def test_reference_encoder():
     """By hand: ties to the even code, saturation at the type's end, the power that keeps the largest from rounding past 6."""
     x = np.zeros((1, 32))
