@@ -293,13 +293,14 @@ struct Kv4Params {
     const unsigned char *codes[2], *scales[2];  // K, V
     long long c_b, c_h, c_s, s_b, s_h, s_s;
     const int* lens;
-    float* ws;        // partial O [nparts][rows][D], then m [nparts][rows], l [nparts][rows], then {first split, splits} [B] or the plan
+    float* ws;        // partial O [nparts][rows][D], then m [nparts][rows], l [nparts][rows], then {first place, splits} [B] or the plan
     int B, Hq, Hkv, Sq, S;
     int R;            // query rows per (sequence, K/V head)
     int rows;         // of a chunk of them, a multiple of 16
     int nchunks;
     int aim;          // splits of all sequences together that fill the chip
     int P;            // and at most: KV_FINER aim + B, or B where every sequence is one split (the grid)
+    int slots;        // places for partials, per K/V head and chunk: only parts of a sequence that is split have one, at most 4 aim
     int least;        // blocks per split, at least
     int merges;       // sequences that the merge looks at: B, or, with a plan, those that are split: at most KV_FINER aim
     int planned;
@@ -318,22 +319,22 @@ __device__ __forceinline__ int kv4_len(const Kv4Params& p, int b)
 }
 
 struct Kv4Split {
-    int b, split, nsplit, first;  // sequence, its split, its splits, the index of its first split
-    int len, begin, end;          // keys, blocks
+    int b, split, nsplit, slot;  // sequence, its split, its splits, the place of this one's partial (several splits)
+    int len, begin, end;         // keys, blocks
 
-    __device__ __forceinline__ void cut(int x)  // from b, nsplit, first and len
+    __device__ __forceinline__ void cut()  // from split, nsplit and len
     {
         const int all = ((len - 1) >> KV_SHIFT) + 1, each = (all + nsplit - 1) / nsplit;
-        split = x - first;
         begin = split * each < all ? split * each : all;
         end = begin + each < all ? begin + each : all;
     }
 };
 
-// The plan as its kernel leaves it: splits P, then merges, each {sequence or -1, its first split, its splits, its keys}.
+// The plan as its kernel leaves it: splits P, each {sequence or -1, split and splits << 16, the place of its partial, keys}, then
+// merges, each {sequence or -1, the place of its first partial, splits, 0}.  (A sequence has at most KV_FINER aim + 1 splits.)
 __device__ __forceinline__ i32x4_t* kv4_plan_of(const Kv4Params& p, int D)
 {
-    return (i32x4_t*)(p.ws + (size_t)p.Hkv * p.nchunks * p.P * p.rows * (D + 2));
+    return (i32x4_t*)(p.ws + (size_t)p.Hkv * p.nchunks * p.slots * p.rows * (D + 2));
 }
 
 // Parts of a sequence of n blocks (-1: there is no sequence), rcp = 1 / L.  Need not be the exact quotient: its blocks are dealt out
@@ -348,7 +349,8 @@ __device__ __forceinline__ int kv4_parts(int n, float rcp)
 //   L is the mean, total / aim, where that makes no more than `aim` parts, as it does for lengths that are alike; or up to twice
 // the mean if that keeps them to `aim`, found by halving to a sixteenth (a further round of work-groups costs more than longer parts,
 // a longer search more than the shorter parts give); or, with many sequences or one that is most of the batch, half the mean
-// (at most 2 aim + B parts).  32/8 heads, D = 128, us with L = total / max(aim, B) always, the mean, half and a quarter of it: one of
+// (at most 2 aim + B parts).  A sequence of m > 1 parts has more than (m - 1) L blocks, at least m L / 2, so that the parts of those
+// that are split are at most 2 total / L, 4 aim.  32/8 heads, D = 128, us with L = total / max(aim, B) always, the mean, half and a quarter of it: one of
 // 30000 among 47 of 100 keys 115 / 17.5 / 18.1 / 22.1, 100 of 1 to 8192 103 / 108 / 98 / 91, 64 of 5000 60.5 / 64.1 / 63.9 / 68.1.
 template <typename Count>
 __device__ __forceinline__ int kv4_part_blocks(const Kv4Params& p, int total, Count&& count)
@@ -380,21 +382,24 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
         return false;  // the grid is rounded up to eights
     if (p.P == p.B) {  // short caches, or many: a part each
         out->b = x;
-        out->first = x;
+        out->split = 0;
         out->nsplit = 1;
+        out->slot = 0;
         out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, x));
-        out->cut(x);
+        out->cut();
         return true;
     }
     if (p.planned) {
         const i32x4_t e = kv4_plan_of(p, D)[x];
         out->b = __builtin_amdgcn_readfirstlane(e.x);
-        out->first = __builtin_amdgcn_readfirstlane(e.y);
-        out->nsplit = __builtin_amdgcn_readfirstlane(e.z);
+        const int y = __builtin_amdgcn_readfirstlane(e.y);
+        out->split = y & 0xffff;
+        out->nsplit = y >> 16;
+        out->slot = __builtin_amdgcn_readfirstlane(e.z);
         out->len = __builtin_amdgcn_readfirstlane(e.w);
         if (out->b < 0)
             return false;
-        out->cut(x);
+        out->cut();
         return true;
     }
     const int nch = (p.B + 63) >> 6;
@@ -413,21 +418,25 @@ __device__ __forceinline__ bool kv4_split(const Kv4Params& p, int x, int lane, K
         return wave_sum(sum);
     });
     const float rcp = __builtin_amdgcn_rcpf((float)L);
-    int before = 0;
+    int before = 0, slots_before = 0;
     for (int c = 0; c < nch; ++c) {
         const int m = kv4_parts(of(c), rcp);
-        const int incl = wave_scan(m) + before;
+        int sum[2] = {m, m > 1 ? m : 0};
+        wave_scan(sum);
+        const int incl = sum[0] + before;
         const unsigned long long mask = __builtin_amdgcn_ballot_w64(incl > x);
         if (mask == 0) {
             before = __builtin_amdgcn_readlane(incl, 63);
+            slots_before += __builtin_amdgcn_readlane(sum[1], 63);
             continue;
         }
         const int src = __builtin_ctzll(mask);
         out->b = c * 64 + src;
         out->nsplit = __builtin_amdgcn_readlane(m, src);
-        out->first = __builtin_amdgcn_readlane(incl, src) - out->nsplit;
+        out->split = x - (__builtin_amdgcn_readlane(incl, src) - out->nsplit);
+        out->slot = slots_before + __builtin_amdgcn_readlane(sum[1], src) - out->nsplit + out->split;  // (one part: not used)
         out->len = __builtin_amdgcn_readfirstlane(kv4_len(p, out->b));
-        out->cut(x);
+        out->cut();
         return true;
     }
     return false;
@@ -484,31 +493,32 @@ __global__ __launch_bounds__(PLAN_THREADS) void naut_decode_kv4_plan_kernel(cons
     });
     const float rcp = __builtin_amdgcn_rcpf((float)L);
     i32x4_t* const plan = kv4_plan_of(p, D);
-    int parts = 0, merges = 0;  // of the sequences so far
+    int parts = 0, merges = 0;  // of the sequences so far; merges: sequences that are split, and their parts << 16 (at most 4 aim <= 1024)
     for (int b0 = 0; b0 < p.B; b0 += PLAN_THREADS) {
-        const int b = b0 + tid, len = len_of(b), m = kv4_parts(blocks(len), rcp), s = m > 1;
+        const int b = b0 + tid, len = len_of(b), m = kv4_parts(blocks(len), rcp), s = m > 1 ? m << 16 | 1 : 0;
         const int m_incl = wave_scan(m), s_incl = wave_scan(s);
         int mb, sb, ma, sa;
         over_waves(__builtin_amdgcn_readlane(m_incl, 63), __builtin_amdgcn_readlane(s_incl, 63), &mb, &sb, &ma, &sa);
-        const int first = parts + mb + m_incl - m, at = merges + sb + s_incl - s;
+        const int first = parts + mb + m_incl - m, at = merges + sb + s_incl - s, slot = at >> 16;
         if (m > 0 && first < p.P)
-            plan[first] = i32x4_t{b, first, m, len};
-        if (s && at < p.merges)
-            plan[p.P + at] = i32x4_t{b, first, m, len};
+            plan[first] = i32x4_t{b, m << 16, slot, len};
+        if (s != 0 && (at & 0xffff) < p.merges)
+            plan[p.P + (at & 0xffff)] = i32x4_t{b, slot, m, 0};
         // the other parts of a sequence, by the wavefront
-        for (unsigned long long left = __builtin_amdgcn_ballot_w64(s); left != 0; left &= left - 1) {
+        for (unsigned long long left = __builtin_amdgcn_ballot_w64(s != 0); left != 0; left &= left - 1) {
             const int src = __builtin_ctzll(left);
-            const i32x4_t e = {b0 + wave * 64 + src, __builtin_amdgcn_readlane(first, src), __builtin_amdgcn_readlane(m, src), __builtin_amdgcn_readlane(len, src)};
-            for (int i = 1 + lane; i < e.z; i += 64)
-                if (e.y + i < p.P)
-                    plan[e.y + i] = e;
+            const int first_s = __builtin_amdgcn_readlane(first, src), m_s = __builtin_amdgcn_readlane(m, src);
+            const int slot_s = __builtin_amdgcn_readlane(slot, src), len_s = __builtin_amdgcn_readlane(len, src);
+            for (int i = 1 + lane; i < m_s; i += 64)
+                if (first_s + i < p.P)
+                    plan[first_s + i] = i32x4_t{b0 + wave * 64 + src, m_s << 16 | i, slot_s + i, len_s};
         }
         parts += __builtin_amdgcn_readfirstlane(ma);
         merges += __builtin_amdgcn_readfirstlane(sa);
     }
     for (int x = parts + tid; x < p.P; x += PLAN_THREADS)
         plan[x] = i32x4_t{-1, 0, 0, 0};
-    for (int x = merges + tid; x < p.merges; x += PLAN_THREADS)
+    for (int x = (merges & 0xffff) + tid; x < p.merges; x += PLAN_THREADS)
         plan[p.P + x] = i32x4_t{-1, 0, 0, 0};
 }
 
@@ -794,13 +804,13 @@ __global__ __launch_bounds__(kv4_waves(D, RT) * 64) void naut_decode_kv4_kernel(
     }
     __syncthreads();
     const int rows = p.R - row0 < p.rows ? p.R - row0 : p.rows;
-    const int part = (hk * p.nchunks + chunk) * p.P + x_of;
-    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
+    const int part = (hk * p.nchunks + chunk) * p.slots + sp.slot;  // not used by a sequence of one part
+    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.slots;
     float* const ws_m = p.ws + nparts * p.rows * D;
     float* const ws_l = ws_m + nparts * p.rows;
     if (sp.split == 0 && chunk == 0 && hk == 0 && tid == 0 && p.P > p.B && !p.planned) {  // for the merge
         int* const at = (int*)(ws_l + nparts * p.rows) + 2 * b;
-        at[0] = sp.first;
+        at[0] = sp.slot;
         at[1] = sp.nsplit;
     }
     for (int x = tid; x < rows * Q4; x += NW * 64) {
@@ -842,7 +852,7 @@ __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(c
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int row = blockIdx.x, hk = blockIdx.y;
     const int chunk = row / p.rows, r = row % p.rows;
-    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.P;
+    const size_t nparts = (size_t)p.Hkv * p.nchunks * p.slots;
     const float* ws_m = p.ws + nparts * p.rows * D;
     const float* ws_l = ws_m + nparts * p.rows;
     int b = blockIdx.z, first, nsplit;
@@ -858,7 +868,7 @@ __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(c
     }
     if (nsplit <= 1)
         return;  // stored already, or no sequence
-    const size_t part0 = (size_t)(hk * p.nchunks + chunk) * p.P + first;
+    const size_t part0 = (size_t)(hk * p.nchunks + chunk) * p.slots + first;
     ws_m += part0 * p.rows + r;
     ws_l += part0 * p.rows + r;
     const float* const ws_o = p.ws + (part0 * p.rows + r) * D;
@@ -925,7 +935,7 @@ __global__ __launch_bounds__(MRG_WAVES * 64) void naut_decode_kv4_merge_kernel(c
 
 constexpr int kv4_width(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
 
-// Fills in what the sizes decide: R, rows, nchunks, P, least, and the workspace.
+// Fills in what the sizes decide: R, rows, nchunks, P, slots, least, and the workspace.
 bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t* bytes)
 {
     const long long R = (long long)(Hq / Hkv) * Sq;
@@ -945,11 +955,12 @@ bool kv4_plan(int B, int Hq, int Hkv, int Sq, int S, int D, Kv4Params* p, size_t
     p->nchunks = (int)nchunks;
     p->aim = (int)aim;
     p->P = (int)P;
+    p->slots = (int)(P < 4 * aim ? P : 4 * aim);  // P: a few sequences
     p->least = (int)least;
     p->planned = P > B && B >= KV_PLANNED;
     p->merges = p->planned && B > KV_FINER * aim ? (int)aim * KV_FINER : B;
     const size_t ints = p->planned ? ((size_t)P + p->merges) * 4 : (size_t)B * 2;
-    *bytes = P > B ? ((size_t)Hkv * nchunks * P * rows * (kv4_width(D) + 2) * sizeof(float) + ints * sizeof(int) + 15) / 16 * 16 : 16;
+    *bytes = P > B ? ((size_t)Hkv * nchunks * p->slots * rows * (kv4_width(D) + 2) * sizeof(float) + ints * sizeof(int) + 15) / 16 * 16 : 16;
     return true;
 }
 

@@ -218,6 +218,29 @@ def test_many_unlike_sequences(B):
     run(2, 1, 1, 2080, 32, [0] * B, seed=15)
 
 
+@pytest.mark.parametrize("B,Hkv,S", [(63, 8, 3000), (40, 8, 2500), (300, 1, 2240), (400, 1, 2240), (1025, 2, 2100), (3, 1, 30000), (70, 3, 2600), (5, 300, 600)])
+def test_partials_stay_in_the_workspace(B, Hkv, S):
+    """Sequences that are all split, nearly all, and few of many: nothing is written behind the workspace, whose bytes are not a number."""
+    lens = [S] * B if B < 1000 else [S if b % 16 == 0 else 3 for b in range(B)]
+    print("partials", B, Hkv, S, flush=True)
+    D = 32
+    cache = filled(B, Hkv, S, D, lens, "bf16", seed=17)
+    q = torch.randn((B, Hkv, 1, D), device="cuda", generator=torch.Generator(device="cuda").manual_seed(18)).to(torch.bfloat16)
+    o, lse = torch.empty_like(q), torch.empty((B, Hkv, 1), device="cuda")
+    n = nb.decode_kv4_workspace_bytes(B, Hkv, Hkv, 1, S, D)
+    room = torch.full((n + (1 << 22),), 0xFF, dtype=torch.uint8, device="cuda")
+    nb.naut_attn_decode_kv4(q, o, lse, cache, slots_of(lens), True, 0.2, room[:n])
+    torch.cuda.synchronize()
+    assert (room[n:] == 0xFF).all()
+    some = sorted(set(range(0, B, max(1, B // 40))) | {B - 1})
+    k, v = (su.decode(c[some].cpu().numpy(), s[some].cpu().numpy(), D) for c, s in (cache.tensors[:2], cache.tensors[2:]))
+    qn, on, ln = q[some].double().cpu().numpy(), o[some].double().cpu().numpy(), lse[some].double().cpu().numpy()
+    for i, b in enumerate(some):
+        for h in sorted({0, Hkv // 2, Hkv - 1}):
+            ref = su.reference(qn[i, h], k[i, h, : lens[b]], v[i, h, : lens[b]], 0.2, True)
+            su.check(on[i, h], ln[i, h], ref, "bf16", "bf16", S, "sequence %d head %d" % (b, h))
+
+
 def test_a_plan_in_a_captured_call_follows_the_lengths():
     B, S = 300, 2200
     cache = filled(B, 2, S, 64, [S] * B, "bf16")

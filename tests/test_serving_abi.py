@@ -144,6 +144,14 @@ def test_workspace_where_the_positions_pass_32_bits():
     assert w(65024, 8, 2, 1, 64, 128) == 0       # more sequences than a grid has with the parts of the split ones
 
 
+def test_the_partials_do_not_grow_with_the_sequences():
+    """Sequences of one part have no partial result; what is left is the plan, a few words each."""
+    w = nb.decode_kv4_workspace_bytes
+    for Hq, Hkv, Sq, S, D in ((32, 8, 1, 2304, 128), (8, 1, 1, 2304, 64), (64, 8, 4, 4096, 256), (3, 3, 1, 5000, 96)):
+        assert w(8192, Hq, Hkv, Sq, S, D) - w(1024, Hq, Hkv, Sq, S, D) <= 64 * (8192 - 1024)
+        assert w(60000, Hq, Hkv, Sq, S, D) - w(1024, Hq, Hkv, Sq, S, D) <= 64 * (60000 - 1024)
+
+
 def test_reference_encoder():
     """By hand: ties to the even code, saturation at the type's end, the power that keeps the largest from rounding past 6."""
     x = np.zeros((1, 32))
