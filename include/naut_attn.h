@@ -268,7 +268,9 @@ int naut_attn_fwd_packed(const void* q, const void* k, const void* v, void* o, f
 /*
  * A key/value cache in 4 bits (OCP MXFP4).  A row of D values, D a multiple of 32 up to 256, is held in blocks of 32: value =
  * code * 2^(byte - 127), the codes E2M1 (sign, then the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6), two to a byte with the even
- * element in the low nibble, and one scale byte per block (1 .. 254; 255 is NaN and must not occur).  Row s of head h of
+ * element in the low nibble, and one scale byte per block: 1 .. 252, as naut_kv4_store writes them.  Above, 4 and 6 times 2^126 or
+ * 2^127 pass the range of bf16 and fp32 (a load gives infinities, decode no defined row of o; 255 is NaN), unless the call is one of
+ * NAUT_F16, which bounds every scale.  Row s of head h of
  * sequence b has its D/2 code bytes at codes + b*c_b + h*c_h + s*c_s and its D/32 scale bytes at scales + b*s_b + h*s_h +
  * s*s_s, for K and V alike.  codes are 16-byte aligned, their strides non-negative multiples of 16; the rows of scales
  * are padded to naut_kv4_scale_bytes(D) = 2 (D <= 64), 4 (D <= 128) or 8 bytes (the rest of them is not looked at), to which

@@ -41,7 +41,7 @@ struct Mx<NAUT_BF16> {
     }
     static __device__ __forceinline__ float high(int two) { return __builtin_bit_cast(float, two & (int)0xffff0000); }
     static __device__ __forceinline__ float low(int two) { return __builtin_bit_cast(float, two << 16); }
-    static __device__ __forceinline__ int scale_of(int byte) { return byte; }
+    static __device__ __forceinline__ int scale_of(int byte) { return byte; }  // (none above MOST, by the format of the header)
     static __device__ __forceinline__ f32x4_t mfma(i32x4_t a, i32x4_t b, f32x4_t c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);

@@ -112,6 +112,25 @@ def test_load_of_scales_beyond_f16_stays_finite():
     assert (k[3, 0, :32] == 0).all() and (k[3, 0, 32:] == 6 * 2.0 ** -24).all()
 
 
+def test_load_of_scales_beyond_those_that_a_store_writes():
+    """bf16: what the type holds is exact up to the last scale that is a number, the rest infinite; 252 is the last where all is finite."""
+    cache = new_cache(1, 1, 3, 32)
+    for t in cache.tensors[0::2]:
+        t[0, 0, :, :] = torch.tensor([0x10 * (2 * i + 1) + 2 * i for i in range(8)] * 2, dtype=torch.uint8, device="cuda")
+    for t in cache.tensors[1::2]:
+        t[0, 0, :, 0] = torch.tensor([252, 253, 254], dtype=torch.uint8, device="cuda")
+    k, v = (torch.empty((3, 1, 32), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    nb.naut_kv4_load(k, v, cache, slots_of([0, 1, 2]))
+    codes = np.array(list(range(16)) * 2)
+    signed = np.where(codes < 8, 1.0, -1.0) * su.MAGNITUDES[codes & 7]
+    for i, byte in enumerate((252, 253, 254)):
+        want = signed * 2.0 ** (byte - 127)
+        want = np.where(np.abs(want) < 2.0 ** 128, want, np.copysign(np.inf, want))
+        assert np.isfinite(want).all() == (byte == 252)
+        for x in (k, v):
+            assert np.array_equal(x[i, 0].double().cpu().numpy(), want), byte
+
+
 def filled(B, Hkv, S, D, lens, dtype, seq_major=False, seed=0, magnify=1.0):
     """A cache whose first lens[b] positions hold rows, the rest garbage that is not a number."""
     cache = new_cache(B, Hkv, S, D, seq_major)
