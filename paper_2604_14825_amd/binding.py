@@ -584,7 +584,8 @@ class KV4Cache:
     """A key/value cache in 4 bits: the caller's tensors, checked once.
 
     k_codes, v_codes uint8 [B,Hkv,S,D/2]; k_scales, v_scales uint8 [B,Hkv,S,kv4_scale_bytes(D)]; the last axes contiguous,
-    the others with any strides (a sequence-major cache is `x.transpose(1, 2)`), the same for K and V."""
+    the others with any strides (a sequence-major cache is `x.transpose(1, 2)`), the same for K and V.  Scale bytes are 1 .. 252
+    (powers of two with bias 127); f16 rows and queries hold less, see naut_kv4_load."""
 
     def __init__(self, k_codes, k_scales, v_codes, v_scales):
         import torch
@@ -637,7 +638,10 @@ def naut_kv4_store(k, v, cache, slots, stream=None):
 
 
 def naut_kv4_load(k, v, cache, slots, stream=None):
-    """The reverse of naut_kv4_store: rows of a KV4Cache into k, v [T,Hkv,D].  Rows whose slot is skipped are left as they are."""
+    """The reverse of naut_kv4_store: rows of a KV4Cache into k, v [T,Hkv,D].  Rows whose slot is skipped are left as they are.
+
+    bf16 rows are exactly what the cache holds.  In f16 a cache that was stored from bf16 may hold more than the type: scales
+    above 2^13 count as 2^13, so that those blocks come out smaller, and values below the type's range round."""
     _kv4_rows(lib().naut_kv4_load, k, v, cache, slots, stream)
 
 
@@ -650,7 +654,7 @@ def naut_attn_decode_kv4(q, o, lse, cache, lens, causal: bool, scale: float, wor
     """Decode-time attention over a KV4Cache: q,o [B,Hq,Sq,D] (the last Sq positions of each sequence; the last axis
     contiguous), lse contiguous fp32 [B,Hq,Sq] or None, lens contiguous int32 device tensor [B], the keys that each sequence
     has (None: S each), workspace contiguous, at least decode_kv4_workspace_bytes(...) bytes.  Enqueues on `stream`; the
-    lengths are read on the GPU."""
+    lengths are read on the GPU.  With f16 queries the cache's values count as naut_kv4_load would give them in f16."""
     import torch
     device = _one_device(q, o, workspace, cache.tensors[0])
     if q.dim() != 4 or o.dim() != 4:

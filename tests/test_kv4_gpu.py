@@ -131,6 +131,32 @@ def test_load_of_scales_beyond_those_that_a_store_writes():
             assert np.array_equal(x[i, 0].double().cpu().numpy(), want), byte
 
 
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_f16_decode_takes_the_values_that_a_load_gives(D):
+    """A cache stored from bf16 with scales above and below what f16 holds: decode in f16 is attention over its rows loaded in f16."""
+    gen = torch.Generator(device="cuda").manual_seed(19)
+    S, n = 300, 257
+    k, v = (torch.randn((S, 2, D), device="cuda", generator=gen) for _ in range(2))
+    k[:, :, 32:64] *= 1e-8
+    v[::7] *= 2.0 ** 16     # scales of 2^14 and more
+    v[:, :, :32] *= 1e-8
+    cache = new_cache(1, 2, S, D)
+    every = slots_of(np.arange(S))
+    nb.naut_kv4_store(k.to(torch.bfloat16), v.to(torch.bfloat16), cache, every)
+    assert (cache.tensors[3][..., : D // 32] > 140).any()
+    k16, v16 = (torch.empty((S, 2, D), device="cuda", dtype=torch.float16) for _ in range(2))
+    nb.naut_kv4_load(k16, v16, cache, every)
+    q = torch.randn((1, 4, 1, D), device="cuda", generator=gen).to(torch.float16)
+    o, lse = torch.empty((1, 4, 1, D), device="cuda"), torch.empty((1, 4, 1), device="cuda")
+    ws = torch.empty(nb.decode_kv4_workspace_bytes(1, 4, 2, 1, S, D), dtype=torch.uint8, device="cuda")
+    nb.naut_attn_decode_kv4(q, o, lse, cache, slots_of([n]), True, D ** -0.5, ws)
+    torch.cuda.synchronize()
+    qn, kn, vn = (x.double().cpu().numpy() for x in (q, k16, v16))
+    for h in range(4):
+        ref = su.reference(qn[0, h], kn[:n, h // 2], vn[:n, h // 2], D ** -0.5, True)
+        su.check(o[0, h].double().cpu().numpy(), lse[0, h].double().cpu().numpy(), ref, "f16", "f32", n, "head %d" % h)
+
+
 def filled(B, Hkv, S, D, lens, dtype, seq_major=False, seed=0, magnify=1.0):
     """A cache whose first lens[b] positions hold rows, the rest garbage that is not a number."""
     cache = new_cache(B, Hkv, S, D, seq_major)
