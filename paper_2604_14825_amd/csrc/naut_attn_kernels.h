@@ -70,6 +70,7 @@ constexpr int HEADS_AT_ONCE = NAUT_HAO;  // (batch, head) pairs an XCD works on 
 constexpr int NWAVES = 4;
 constexpr int NTHREADS = NWAVES * 64;
 constexpr float RESCALE_TAU = 6.0f;  // log2 units
+constexpr float P_LIMIT_SHORT = 24.0f;  // Params::p_limit where loops are short (see launch)
 
 // The kernels are compiled for head dimensions 64, 80, 96, 128, 192 and 256; a head in between runs on the next
 // wider one.  In LDS a row of K or V always takes 64, 128 or 256 values, so that the swizzles (which need a power
@@ -834,12 +835,18 @@ inline int wide_variant(int S, long long nbh, int D, int causal)
     return 4 * r4 <= 5 * r8 || (r4 == 4 && r8 == 3 && D == 256 && S >= 1024) ? V_BM128 : V_W8Q32;
 }
 
+// From which length on key loops are long, D <= 128: 2048 keys on average with the mask, 1024 without, 8192 at D = 64.
+inline int long_length(int D, int causal)
+{
+    const int avg_keys = D <= 64 ? 8192 : causal ? 2048 : 1024;
+    return causal ? 2 * avg_keys - 1 : avg_keys;
+}
+
 // Whether a shape of D <= 128 runs long key loops with whole rounds of 256-query work-groups.
 inline bool long_loops(int S, long long nbh, int D, int causal)
 {
     const long long wg256 = nbh * ((S + BM2 - 1) / BM2);
-    const int avg_keys = causal ? (S + 1) / 2 : S;
-    return wg256 >= 256 && (D > 64 ? avg_keys >= (causal ? 2048 : 1024) : avg_keys >= 8192 && wg256 < 1024);
+    return wg256 >= 256 && S >= long_length(D, causal) && (D > 64 || wg256 < 1024);
 }
 
 // Key groups of the shapes without long loops (D: the compiled width): four for grids of at most 256 work-groups of 64
@@ -983,7 +990,7 @@ int launch(Params p, int causal, hipStream_t stream)
     // rows that few keys dominate.  Relative error against 64 bits over that of kernel 1 with as many key groups (bf16, f32
     // O, 256 shapes) with limits of 32, 24 and 16: four times the usual scale 0.99, 0.94, 0.92; twice 0.97, 0.95, 0.91; usual
     // 0.997, 0.997, 0.996.  24 costs 0.1 % of the time on N(0,1) inputs, 16 1.2 %, 8 up to 13 %.
-    p.p_limit = long_loops(p.S, nbh, D, causal) ? In<DT_IN>::P_LIMIT : 24.0f;  // by shape, whatever form is named
+    p.p_limit = long_loops(p.S, nbh, D, causal) ? In<DT_IN>::P_LIMIT : P_LIMIT_SHORT;  // by shape, whatever form is named
     if (variant < 0)
         return fail(NAUT_ERR_UNSUPPORTED, "NAUT_ATTN_VARIANT names no kernel variant (w8q32, w4q64, w4q32, w4q32g2, bm128, bm128g1, bm128g2 or bm128g4)");
     const long long nblocks = nbh * (groups == 4 ? (p.S + 63) / 64 : variant == V_BM128 || variant == V_W4Q32 ? p.nqt : p.nqt2);

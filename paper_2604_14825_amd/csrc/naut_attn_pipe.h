@@ -179,7 +179,9 @@ __global__ __launch_bounds__(NWV * NG * 64, (pipe_waves_per_simd<D, QH, NWV, NG>
     }
     const int hk = hq / (p.Hq / p.Hkv);
     const float c = p.c;
-    const float p_limit = p.p_limit;
+    float p_limit = p.p_limit;
+    if constexpr (PACKED)
+        p_limit = Sk >= p.long_from ? p_limit : P_LIMIT_SHORT;
     float c_v = c;  // copy held in a vector register: an FMA with a scalar-register operand issues at the slower rate
     asm volatile("" : "+v"(c_v));
 

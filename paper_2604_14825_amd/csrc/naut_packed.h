@@ -20,6 +20,7 @@ struct PackedParams : Params {  // batch strides, S and the counts of tiles are 
     unsigned g_inv;  // ceil(2^22 / g)
     int pos_per_tile;  // positions of a tile where they are whole, otherwise 0
     int all_keys;      // no mask: every query sees every key, as if Sk - 1 keys came before the first one's own
+    int long_from;     // keys from which on a sequence may have p_limit, shorter ones P_LIMIT_SHORT
     int by_level;      // the tiles go by level, not by sequence (see packed_tile; at most PACKED_BY_LEVEL sequences)
     int class_of[6];   // levels at which a class of tiles ends, falling
 };

@@ -67,7 +67,11 @@ template <int D, int DT_IN, int DT_OUT>
 int launch_packed(PackedParams p, int causal, hipStream_t stream)
 {
     const int mean = (int)(((long long)(p.Tk > p.Tq ? p.Tk : p.Tq) + p.n - 1) / p.n);
-    p.p_limit = long_loops(mean, (long long)p.n * p.Hq, D, causal) ? In<DT_IN>::P_LIMIT : 24.0f;  // as in launch(), for a sequence of mean length
+    // As in launch(), for a sequence of mean length; shorter ones beside long ones keep the limit of short loops, as their O would be
+    // less exact for the company (error of O against 64 bits beside six sequences of 16384, D = 128, over that without them: 1000
+    // keys, some of them outliers 1.42, 300 and 1000 keys at three times the usual scale 1.15 and 1.19).
+    p.p_limit = long_loops(mean, (long long)p.n * p.Hq, D, causal) ? In<DT_IN>::P_LIMIT : P_LIMIT_SHORT;
+    p.long_from = long_length(D, causal);
     p.by_level = p.n > 1 && p.n < (packed_more_keys(p) ? PACKED_BY_LEVEL + 1 : 32);  // both sides' times are at packed_tile
     int groups;
     const int form = packed_form(p, D, causal, &groups);

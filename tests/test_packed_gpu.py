@@ -259,6 +259,29 @@ def test_sequences_that_share_rows_are_right_or_left_out(turns, length, causal, 
     assert not left.all()
 
 
+@pytest.mark.parametrize("variant", ["w4q32", "w4q32g2", "w8q32", "bm128g4"])
+@pytest.mark.parametrize("D,causal,far", [(128, True, 8200), (128, False, 4100), (80, True, 8200), (64, False, 16500)])
+def test_a_sequence_is_as_exact_beside_long_ones(D, causal, far, variant, monkeypatch):
+    """Keys of which a few are much larger move the reference maximum: how far it may lag is a matter of the sequence's own length,
+    and so the same kernel gives the same bits whatever else is in the batch."""
+    monkeypatch.setenv("NAUT_ATTN_VARIANT", variant)
+    print("beside long ones", D, causal, variant, flush=True)
+    lens, Hq, Hkv = [300, 1000, 77], 2 if D == 64 else 8, 2 if D == 64 else 8
+    gen = torch.Generator(device="cuda").manual_seed(20)
+    T, more = sum(lens), [far] * (4 if D == 64 else 3)
+    q, k, v = (torch.randn((T + sum(more), H, D), device="cuda", generator=gen) for H in (Hq, Hkv, Hkv))
+    k = torch.where(torch.rand((T + sum(more), Hkv, 1), device="cuda", generator=gen) < 1 / 256, 6 * k, k)
+    q, k, v = (x.to(torch.bfloat16) for x in (q, k, v))
+    out = []
+    for ls in (lens, lens + more):
+        n = sum(ls)
+        o, lse = torch.full((n, Hq, D), 7.0, device="cuda"), torch.full((Hq, n), 7.0, device="cuda")
+        nb.naut_attn_fwd_packed(q[:n], k[:n], v[:n], o, lse, offsets(ls), offsets(ls), causal, D ** -0.5)
+        torch.cuda.synchronize()
+        out.append((o[:T], lse[:, :T]))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
+
+
 def test_calls_repeat_bit_for_bit_and_on_another_stream():
     a, la = run([333, 1, 90], None, 8, 2, 128, True, seed=10)
     s = torch.cuda.Stream()
