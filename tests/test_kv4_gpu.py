@@ -388,6 +388,64 @@ def test_two_captured_calls_share_a_workspace_in_turn_and_follow_the_lengths():
             su.check(os[i].double().cpu().numpy(), None, ref, "bf16", "bf16", S, str(now))
 
 
+@pytest.mark.parametrize("B,S", [(1, 1), (7, 1), (3, 31), (300, 2)])
+def test_the_smallest_caches(B, S):
+    for D in (32, 128, 256):
+        run(4, 2, 1, S, D, [S] * B, seed=21)
+        run(4, 2, 3, S, D, [b % (S + 1) for b in range(B)], seed=21)
+
+
+def test_a_captured_step_follows_slots_and_lengths():
+    """One graph of a step of generation: new rows into the cache, attention over it, the rows back; slots and lengths change between replays,
+    a finished sequence's slot is skipped, and eager work runs in between."""
+    B, Hq, Hkv, S, D = 4, 8, 2, 700, 128
+    lens0 = [600, 1, 33, 0]
+    cache = filled(B, Hkv, S, D, lens0, "bf16", seed=22)
+    gen = torch.Generator(device="cuda").manual_seed(23)
+    rows = lambda H: torch.randn((B, H, D), device="cuda", generator=gen).to(torch.bfloat16)
+    q, k, v = rows(Hq), rows(Hkv), rows(Hkv)
+    o, lse = torch.empty((B, Hq, 1, D), device="cuda", dtype=torch.bfloat16), torch.empty((B, Hq, 1), device="cuda")
+    k_back, v_back = torch.empty_like(k), torch.empty_like(v)
+    slots, lens = slots_of([-1] * B), slots_of(lens0)
+    ws = torch.empty(nb.decode_kv4_workspace_bytes(B, Hq, Hkv, 1, S, D), dtype=torch.uint8, device="cuda")
+
+    def step():
+        nb.naut_kv4_store(k, v, cache, slots)
+        nb.naut_attn_decode_kv4(q.unsqueeze(2), o, lse, cache, lens, True, 0.09, ws)
+        nb.naut_kv4_load(k_back, v_back, cache, slots)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    have = list(lens0)
+    for turn in range(5):
+        runs = [b != turn for b in range(B)]  # one sequence sits out
+        slots.copy_(slots_of([b * S + have[b] if runs[b] else -1 for b in range(B)]))
+        have = [n + r for n, r in zip(have, runs)]
+        lens.copy_(slots_of(have))
+        for x, H in ((q, Hq), (k, Hkv), (v, Hkv)):
+            x.copy_(rows(H))
+        k_back.fill_(7.0)
+        v_back.fill_(7.0)
+        before = [t.clone() for t in cache.tensors]
+        graph.replay()
+        torch.cuda.synchronize()
+        for b in range(B):
+            for i, x in enumerate((k, v)):
+                codes, scales = su.encode(x[b].double().cpu().numpy(), "bf16")
+                for j, new in ((2 * i, codes), (2 * i + 1, scales)):
+                    if runs[b]:
+                        before[j][b, :, have[b] - 1, : new.shape[-1]] = torch.tensor(new, device="cuda")
+                    assert torch.equal(cache.tensors[j][b], before[j][b]), (turn, b)
+        values = held(cache)
+        for b in range(B):
+            for x, want in zip((k_back, v_back), values):
+                got = x[b].double().cpu().numpy()
+                assert np.array_equal(got, want[b, :, have[b] - 1]) if runs[b] else (got == 7.0).all()
+        su.check(o.double().cpu().numpy(), lse.double().cpu().numpy(), reference(q.unsqueeze(2), cache, have, 0.09, True), "bf16", "bf16", S, "turn %d" % turn)
+
+
 def test_a_cache_past_4_gib():
     """Offsets that pass 32 bits: far-apart positions, and the last sequences of a large cache."""
     B, Hkv, S, D, step = 2, 1, 1100, 64, 1 << 22

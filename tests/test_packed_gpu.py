@@ -282,6 +282,45 @@ def test_a_sequence_is_as_exact_beside_long_ones(D, causal, far, variant, monkey
     assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
 
 
+def test_as_many_sequences_as_a_call_takes():
+    """2^20 of them, of one row or none (O is V and lse the score) but for one: a grid of three axes."""
+    n, D = 1 << 20, 8
+    rng = np.random.default_rng(21)
+    lens = (rng.random(n) < 0.3).astype(np.int64)
+    lens[n // 2] = 300
+    gen = torch.Generator(device="cuda").manual_seed(21)
+    T = int(lens.sum())
+    print("sequences", n, "rows", T, flush=True)
+    q, k, v = (torch.randn((T + 5, 2, D), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
+    o, lse = torch.full((T + 5, 2, D), 7.0, device="cuda"), torch.full((2, T + 5), 7.0, device="cuda")
+    cu = offsets(lens)
+    nb.naut_attn_fwd_packed(q, k, v, o, lse, cu, cu, True, 0.25)
+    torch.cuda.synchronize()
+    assert (o[T:] == 7.0).all() and (lse[:, T:] == 7.0).all()
+    a = int(lens[: n // 2].sum())
+    one = torch.ones(T, dtype=torch.bool, device="cuda")
+    one[a : a + 300] = False
+    assert torch.equal(o[:T][one], v[:T][one].float())
+    score = (q.double() * k.double()).sum(-1)[:T][one] * 0.25
+    assert float((lse.T[:T][one].double() - score).abs().max()) <= 8 * 2.0 ** -24 * 40 * 0.25 + 4 * 2.0 ** -23 * 12  # su.check's, |q.k| <= 40
+    ref = reference(q[a : a + 300], k[a : a + 300], v[a : a + 300], [300], [300], 0.25, True)
+    su.check(o[a : a + 300].double().cpu().numpy(), lse[:, a : a + 300].T.double().cpu().numpy(), ref, "bf16", "f32", 300, "the long one")
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_without_lse(D):
+    gen = torch.Generator(device="cuda").manual_seed(22)
+    q, k, v = (torch.randn((300, 4, D), device="cuda", generator=gen).to(torch.bfloat16) for _ in range(3))
+    cu_q, cu_k = offsets([100, 40, 160]), offsets([100, 3, 197])   # the second with rows that see nothing
+    out = []
+    for lse in (torch.empty((4, 300), device="cuda"), None):
+        o = torch.empty_like(q)
+        nb.naut_attn_fwd_packed(q, k, v, o, lse, cu_q, cu_k, True, 0.1)
+        out.append(o)
+    torch.cuda.synchronize()
+    assert torch.equal(*out)
+
+
 def test_calls_repeat_bit_for_bit_and_on_another_stream():
     a, la = run([333, 1, 90], None, 8, 2, 128, True, seed=10)
     s = torch.cuda.Stream()
