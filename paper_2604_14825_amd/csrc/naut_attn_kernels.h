@@ -230,21 +230,17 @@ __global__ __launch_bounds__(NWV * NG * 64, D > 128 ? 1 : 2) void naut_fwd_kerne
     int pos_end = 0;                 // and the position behind its last row's
     if constexpr (PACKED) {
         static_assert(CAUSAL, "no mask is one that leaves every key: p.all_keys");
-        const PackedTile t = packed_tile<BM>(p, lane);
-        if (t.qt < 0)
+        PackedTile t;
+        if (!packed_start<BM, DT_OUT == NAUT_F32 ? 4 : 2>(p, lane, tid, NWV * NG * 64, t))
             return;
         qt = t.qt;
         hq = t.hk * p.g;
         Sq = t.rows;
         Sk = t.Sk;
-        ahead = p.all_keys ? Sk - 1 : Sk - t.Sq;
-        pos0 = p.pos_per_tile ? qt * p.pos_per_tile : qt * BM / p.g;
-        head0 = qt * BM - pos0 * p.g;
-        pos_end = packed_row(p, pos0, head0, (Sq - qt * BM < BM ? Sq - qt * BM : BM) - 1).pos + 1;
-        if (Sk == 0 || pos_end + ahead <= 0) {
-            packed_empty_rows<DT_OUT == NAUT_F32 ? 4 : 2>(p, t, qt * BM, Sq - qt * BM < BM ? Sq - qt * BM : BM, tid, NWV * NG * 64);
-            return;
-        }
+        ahead = t.ahead;
+        pos0 = t.pos0;
+        head0 = t.head0;
+        pos_end = t.pos_end;
         q_first = (long long)t.q0 * p.q_rs;
         k_first = (long long)t.k0 * p.k_rs;
         v_first = (long long)t.k0 * p.v_rs;

@@ -37,6 +37,9 @@ struct PackedTile {
     int q0, k0;      // the sequence's first row of q and of k
     int Sq, Sk;
     int rows;        // Sq * g
+    int ahead;       // keys before the first query's own
+    int pos0, head0; // position and head (of the g) of the tile's first row
+    int pos_end;     // the position behind its last row's
 };
 
 // Position and head (of the g) of the row x of a tile whose first row is position `pos` of head `head`; x + head < 1280 (BM + g),
@@ -277,6 +280,25 @@ __device__ __forceinline__ void packed_empty_rows(const PackedParams& p, const P
         if (p.lse != nullptr && x % pieces == 0)
             p.lse[(size_t)(t.hk * p.g + r % p.g) * p.Tq + t.q0 + r / p.g] = -INFINITY;
     }
+}
+
+// The work-group's tile of BM rows with where it starts and ends; false: there is none for it, or one whose rows see nothing, done here.
+template <int BM, int OUTB>
+__device__ __forceinline__ bool packed_start(const PackedParams& p, int lane, int tid, int threads, PackedTile& t)
+{
+    t = packed_tile<BM>(p, lane);
+    if (t.qt < 0)
+        return false;
+    const int first = t.qt * BM, count = t.rows - first < BM ? t.rows - first : BM;
+    t.ahead = p.all_keys ? t.Sk - 1 : t.Sk - t.Sq;
+    t.pos0 = p.pos_per_tile ? t.qt * p.pos_per_tile : first / p.g;
+    t.head0 = first - t.pos0 * p.g;
+    t.pos_end = packed_row(p, t.pos0, t.head0, count - 1).pos + 1;
+    if (t.Sk == 0 || t.pos_end + t.ahead <= 0) {
+        packed_empty_rows<OUTB>(p, t, first, count, tid, threads);
+        return false;
+    }
+    return true;
 }
 
 }  // namespace naut_k
