@@ -23,9 +23,11 @@ inline long long packed_tiles(const PackedParams& p, int bm)
 // (V_W8Q32) or four (V_W4Q32).  NAUT_ATTN_VARIANT names one as in the rectangular launch (w4q32, w4q32g2, w8q32 or w4q64,
 // bm128g4); a name without a packed form chooses nothing.
 //   The host knows the totals and the number of sequences, not the lengths, so the rule goes by means: tiles of 128 rows (at
-// most), keys per sequence, keys per query.  Fitted to timings of every form in turn over 2914 batches (1 to 64 sequences, eight pairs of
-// head counts, D = 64, 96 and 128, equal, even and log-even lengths, as many keys as queries or up to 8000 more; time over that of
-// the best form, mean): 4 x 32 alone 1.11, the rule 1.02 at D = 64 and 1.01 wider.
+// most), keys per sequence, keys per query.  Fitted to timings of every form in turn over 2914 batches, with the tiles in an earlier
+// order.  On the present kernels, 2725 batches (1 to 256 sequences, eight pairs of head counts, D = 64, 96 and 128, equal, even and
+// log-even lengths, as many keys as queries or up to 8000 more; time over that of the best form): the rule 1.013 on average, 1.19 at the
+// 99th percentile, 1.55 at most; 4 x 32 alone 1.074, 1.55 and 1.66.  It goes by time alone: the key groups that the rectangular rule keeps because
+// they make O more exact (see key_groups) are not kept (error of O up to 1.17 times the rectangular call's, with outlier keys 1.57).
 //   With few tiles the longest loop is what a launch takes, and key groups cut it: up to one tile on every second CU four
 // (1 to 8 heads' prompts of 1000 keys, D = 64 1.2, D = 128 1.1), then two.  Where there are several times as many keys as
 // queries (new turns of long conversations) loops are longer and more unlike, and groups pay up to five rounds of tiles (500 to 900
