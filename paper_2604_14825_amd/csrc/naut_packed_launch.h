@@ -14,7 +14,7 @@ inline long long packed_tiles(const PackedParams& p, int bm)
 {
     const long long rows = (long long)p.Tq * p.g, tiles = (rows + (long long)(bm - 1) * p.n) / bm;
     if (!p.by_level)
-        return rows / bm + p.n;  // the numbers of packed_tile_by_sequence
+        return rows / bm + p.n;  // the numbers of packed_tile_by_sequence, enough for those of packed_tile_by_count
     return tiles < rows ? tiles : rows;
 }
 
@@ -92,9 +92,9 @@ int launch_packed(PackedParams p, int causal, hipStream_t stream)
     if ((tiles + y - 1) / y > 65535 || tiles * p.Hkv > 0x7fffffffLL)
         return fail(NAUT_ERR_UNSUPPORTED, "the heads times the query tiles exceed the grid limits");
     const dim3 grid((unsigned)p.Hkv, (unsigned)y, (unsigned)((tiles + y - 1) / y));
-    // One kernel for both masks: no mask is one that leaves every key.  (Its own instantiation took as long again to compile, a quarter of
-    // the library, and was faster by the few scalar steps before the loop: 32/8 heads, D = 128, 200 of 1 to 64 39.9 us for 41.4, 200
-    // of 1 to 1000 1180 for 1185, 6 of 500 to 4096 392.8 for 392.5.)
+    // One kernel for both masks: no mask is one that leaves every key.  (Its own instantiation takes as long again to compile, a quarter of
+    // the library, and is faster by 0.3 us a round of work-groups: 32/8 heads, D = 128, 64 of 1 to 4 7.2 us for 7.6, 200 of 1 to 64 39.4
+    // for 40.8, 128 of 1 to 200 72.4 for 74.6, 200 of 1 to 1000 1248 for 1245, 6 of 500 to 4096 827 for 829.)
     p.all_keys = !causal;
 #define NAUT_LAUNCH(THREADS, KERNEL, ...) \
     hipLaunchKernelGGL((KERNEL<D, DT_IN, DT_OUT, true, __VA_ARGS__, true>), grid, dim3(THREADS), 0, stream, p)
